@@ -502,6 +502,138 @@ int gmc_prune_static(const gmc_config* cfg, int64_t B, const void* hidden, const
                      const int32_t* pos3d, int64_t N, int64_t T, int64_t K, void* out_hidden, int32_t* out_pos,
                      int32_t* out_idx, const float* nonvis_lse, void* stream);
 
+/*
+ * The paged K/V cache of a compacted prompt: what the cached deployment does
+ * with the boundary sequence and the gathered prefix rows next (App. H
+ * "Index map and physical token accounting"; fixed-support autoregressive
+ * execution, Eq. cond-cached-rollout).  Like gmc_prune_static these entry
+ * points need no context and keep no state between calls: shapes come with
+ * the descriptor, scratch memory and the stream with the call.
+ *
+ * gmc_cache - a host struct that describes one layer's cache of n_seq
+ * sequences; it is read during the call only.  Slot s of sequence b is row
+ * s % page_size of page page_table[b][s / page_size]; a page holds its rows
+ * head by head.  All pointers are device pointers owned by the caller:
+ *   k_pages, v_pages [n_pages][n_kv_heads][page_size][head_dim] dtype, 16-byte
+ *              aligned; the keys as attention uses them (post-norm, post-rotary)
+ *   page_table [n_seq][max_pages] int32.  Entries past a sequence's length are
+ *              not used; a slot on an id outside [0, n_pages) counts as not
+ *              held: attention does not see it, appending leaves it out
+ *   lens       [n_seq] int32, slots held; read as clamped to [0, max_pages *
+ *              page_size].  Slots at and past the length are never read as
+ *              rows, whatever they hold
+ *   seen       [n_seq] int32 or NULL: positions given out so far
+ *   slot_pos   [n_seq][n_kv_heads][max_pages * page_size] int32 or NULL: the
+ *              position of the row in each slot; needed by caches that evict,
+ *              whose slots are in no order (needs seen).  NULL: a slot's
+ *              position is its index
+ *   weights    the same shape, float32, or NULL: the attention weight that
+ *              each row has drawn so far
+ * n_kv_heads divides n_q_heads (<= GMC_CACHE_MAX_HEADS), head_dim is a multiple
+ * of 32 up to 256, page_size a power of two from 16 to 1024; max_pages *
+ * page_size <= 2^24.
+ *
+ * Work goes to `stream` (hipStream_t, NULL: the current device's null
+ * stream), on the stream's own device.  Every call may be captured into a
+ * graph.  Scratch memory is the caller's (256-byte aligned, any content, at
+ * least the bytes that the _bytes function of the call names); calls that may
+ * run at the same time need scratch memory of their own, and calls that change
+ * one cache have to be ordered.  Results are bitwise repeatable.
+ * Errors of all: GMC_ERR_ARG, GMC_ERR_CAPACITY (scratch memory too small),
+ * GMC_ERR_HIP.  The _bytes functions return a negative code for a bad argument.
+ */
+#define GMC_CACHE_MAX_HEADS 256
+typedef struct gmc_cache {
+  int32_t dtype;         /* GMC_F32 or GMC_BF16: pages, q, k, v, out */
+  int32_t n_q_heads, n_kv_heads, head_dim;
+  int32_t page_size;
+  int32_t max_pages;     /* pages of one sequence: columns of page_table */
+  int64_t n_pages;
+  int64_t n_seq;
+  void* k_pages;
+  void* v_pages;
+  const int32_t* page_table;
+  int32_t* lens;
+  int32_t* seen;
+  int32_t* slot_pos;
+  float* weights;
+} gmc_cache;
+
+/*
+ * gmc_cache_append - new rows behind each sequence's last slot: slot lens[b] +
+ * i receives row i of the sequence's n_b rows, its position becomes seen[b] +
+ * i and its weight 0; then lens[b] and seen[b] grow by n_b.
+ *   k, v    rows of n_kv_heads * head_dim elements, k_stride and v_stride
+ *           elements apart (slices of a wider projection); 16-byte aligned,
+ *           strides a multiple of 16 bytes
+ *   rows    rows that k and v hold
+ *   starts  [n_seq + 1] int32: sequence b's rows are [starts[b], starts[b + 1])
+ *           of k and v, at most max_new of them are taken (0 is fine); NULL:
+ *           max_new rows each, one sequence after the other
+ *   src     [n_seq][max_new] int32 or NULL (then starts must be NULL): the
+ *           rows of each sequence to take, as indices into its rows / n_seq
+ *           rows - the keep list of gmc_compact_sequence puts a prefix
+ *           layer's retained K/V into the cache without a gathered copy.
+ *           Indices are clamped
+ * Rows past the capacity are left out, and lens and seen stop there.
+ */
+int gmc_cache_append(const gmc_cache* cache, const void* k, const void* v, int64_t k_stride, int64_t v_stride,
+                     int64_t rows, const int32_t* starts, const int32_t* src, int64_t max_new, void* stream);
+
+/*
+ * gmc_cache_prefill - attention of the n_b newest tokens of each sequence
+ * (their K/V appended before) over the sequence's cache:
+ *   out_i = sum_s exp(l_s - lse_i) v_s,  l_s = scale q_i . k_s,
+ *   lse_i = log sum_s exp l_s
+ * over the held slots s that query i sees.  Query i stands in slot t = lens[b]
+ * - n_b + i; it sees the slots s <= t, with window > 0 those of them whose
+ * position is less than `window` before its own or below `sinks` (the first
+ * tokens of the sequence stay visible).  Query head h reads kv head
+ * h * n_kv_heads / n_q_heads.  A query that sees nothing gives out = 0 and
+ * lse = -inf.  Nothing that a query does not see changes its result, not even
+ * infinities and NaN.
+ *   q       rows of n_q_heads * head_dim elements, q_stride elements apart
+ *           (16-byte aligned, stride a multiple of 16 bytes)
+ *   rows    rows that q and out hold
+ *   starts  [n_seq + 1] int32: sequence b's rows of q; at most max_new of them
+ *           are computed; NULL: max_new each.  Rows of out that belong to no
+ *           sequence are left as they are
+ *   out     [rows][n_q_heads][head_dim] dtype, 16-byte aligned
+ *   lse     [rows][n_q_heads] float32 or NULL
+ */
+int64_t gmc_cache_prefill_bytes(const gmc_cache* cache, int64_t max_new);
+int gmc_cache_prefill(const gmc_cache* cache, const void* q, int64_t q_stride, int64_t rows, const int32_t* starts,
+                      int64_t max_new, float scale, int64_t window, int64_t sinks, void* out, float* lse,
+                      void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * gmc_cache_decode - the same for one new token of every sequence: q
+ * [n_seq][n_q_heads][head_dim] (rows q_stride elements apart), the query of
+ * sequence b in slot lens[b] - 1; out, lse as above with n_seq rows.  A
+ * sequence of length 0 gives out = 0, lse = -inf.  accumulate != 0: adds to
+ * weights[b][h][s] the attention weights exp(l_s - lse) that the query heads
+ * of kv head h put on slot s, for gmc_cache_evict.
+ */
+int64_t gmc_cache_decode_bytes(const gmc_cache* cache, int32_t accumulate);
+int gmc_cache_decode(const gmc_cache* cache, const void* q, int64_t q_stride, float scale, int64_t window,
+                     int64_t sinks, int32_t accumulate, void* out, float* lse, void* workspace,
+                     int64_t workspace_bytes, void* stream);
+
+/*
+ * gmc_cache_evict - every sequence that holds more than `budget` slots keeps
+ * `budget` of them, chosen per kv head: first the rows whose position is
+ * below `sinks` or among the last `recent` positions seen, then those of
+ * largest accumulated weight (ties to the lower slot; NaN counts as lowest).
+ * Attention does not depend on the order of the slots, so only the slots
+ * below the budget whose rows leave are filled: the i-th of them takes the
+ * i-th kept slot at or above the budget - K, V, position and weight.  lens
+ * becomes `budget`.  Needs weights, slot_pos and seen; sinks + recent <=
+ * budget.
+ */
+int64_t gmc_cache_evict_bytes(const gmc_cache* cache, int64_t budget);
+int gmc_cache_evict(const gmc_cache* cache, int64_t budget, int64_t sinks, int64_t recent, void* workspace,
+                    int64_t workspace_bytes, void* stream);
+
 /* Bytes of device workspace the current context holds (0 without one). */
 int64_t gmc_workspace_bytes(void);
 

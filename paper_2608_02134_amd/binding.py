@@ -28,6 +28,7 @@ GMC_MAX_IMAGES = 64
 GMC_AUDIT_ROW, GMC_AUDIT_OUT = 8, 8
 GMC_STATUS_INPUT = 8
 GMC_MAX_GATHER_TENSORS = 64
+GMC_CACHE_MAX_HEADS = 256
 
 _i32, _f32, _i64, _vp = ctypes.c_int32, ctypes.c_float, ctypes.c_int64, ctypes.c_void_p
 
@@ -86,6 +87,14 @@ class GmcDiag(ctypes.Structure):
                 ("batch_margin", ctypes.POINTER(_f32))]
 
 
+class GmcCache(ctypes.Structure):
+    """Mirror of ``gmc_cache``: one layer's paged K/V cache."""
+    _fields_ = [("dtype", _i32), ("n_q_heads", _i32), ("n_kv_heads", _i32), ("head_dim", _i32),
+                ("page_size", _i32), ("max_pages", _i32), ("n_pages", _i64), ("n_seq", _i64),
+                ("k_pages", _vp), ("v_pages", _vp), ("page_table", _vp), ("lens", _vp), ("seen", _vp),
+                ("slot_pos", _vp), ("weights", _vp)]
+
+
 # name -> (restype, argtypes) of every symbol include/gmc.h declares
 SIGNATURES = {
     "gmc_config_default": (None, [ctypes.POINTER(GmcConfig)]),
@@ -114,6 +123,15 @@ SIGNATURES = {
     "gmc_get_diag": (ctypes.c_int, [_i64, ctypes.POINTER(GmcDiag)]),
     "gmc_prune_static": (ctypes.c_int, [ctypes.POINTER(GmcConfig), _i64, _vp, _vp, _vp, _vp, _i64, _i64, _i64,
                                         _vp, _vp, _vp, _vp, _vp]),
+    "gmc_cache_append": (ctypes.c_int, [ctypes.POINTER(GmcCache), _vp, _vp, _i64, _i64, _i64, _vp, _vp, _i64, _vp]),
+    "gmc_cache_prefill_bytes": (_i64, [ctypes.POINTER(GmcCache), _i64]),
+    "gmc_cache_prefill": (ctypes.c_int, [ctypes.POINTER(GmcCache), _vp, _i64, _i64, _vp, _i64, _f32, _i64, _i64, _vp,
+                                         _vp, _vp, _i64, _vp]),
+    "gmc_cache_decode_bytes": (_i64, [ctypes.POINTER(GmcCache), _i32]),
+    "gmc_cache_decode": (ctypes.c_int, [ctypes.POINTER(GmcCache), _vp, _i64, _f32, _i64, _i64, _i32, _vp, _vp, _vp,
+                                        _i64, _vp]),
+    "gmc_cache_evict_bytes": (_i64, [ctypes.POINTER(GmcCache), _i64]),
+    "gmc_cache_evict": (ctypes.c_int, [ctypes.POINTER(GmcCache), _i64, _i64, _i64, _vp, _i64, _vp]),
     "gmc_workspace_bytes": (_i64, []),
     "gmc_last_error": (ctypes.c_char_p, []),
     "gmc_free": (None, []),
@@ -408,6 +426,38 @@ def gmc_prune_static(cfg: GmcConfig, b, hidden, text_q, vis_k, pos3d, n, t, k, o
                                   out_pos, out_idx, nonvis_lse, stream)
 
 
+def gmc_cache_append(cache: GmcCache, k, v, k_stride, v_stride, rows, starts, src, max_new, stream=None) -> int:
+    return lib().gmc_cache_append(ctypes.byref(cache), k, v, k_stride, v_stride, rows, starts, src, max_new, stream)
+
+
+def gmc_cache_prefill_bytes(cache: GmcCache, max_new: int) -> int:
+    return lib().gmc_cache_prefill_bytes(ctypes.byref(cache), max_new)
+
+
+def gmc_cache_prefill(cache: GmcCache, q, q_stride, rows, starts, max_new, scale, window, sinks, out, lse, workspace,
+                      workspace_bytes, stream=None) -> int:
+    return lib().gmc_cache_prefill(ctypes.byref(cache), q, q_stride, rows, starts, max_new, scale, window, sinks, out,
+                                   lse, workspace, workspace_bytes, stream)
+
+
+def gmc_cache_decode_bytes(cache: GmcCache, accumulate: bool) -> int:
+    return lib().gmc_cache_decode_bytes(ctypes.byref(cache), int(accumulate))
+
+
+def gmc_cache_decode(cache: GmcCache, q, q_stride, scale, window, sinks, accumulate, out, lse, workspace,
+                     workspace_bytes, stream=None) -> int:
+    return lib().gmc_cache_decode(ctypes.byref(cache), q, q_stride, scale, window, sinks, int(accumulate), out, lse,
+                                  workspace, workspace_bytes, stream)
+
+
+def gmc_cache_evict_bytes(cache: GmcCache, budget: int) -> int:
+    return lib().gmc_cache_evict_bytes(ctypes.byref(cache), budget)
+
+
+def gmc_cache_evict(cache: GmcCache, budget, sinks, recent, workspace, workspace_bytes, stream=None) -> int:
+    return lib().gmc_cache_evict(ctypes.byref(cache), budget, sinks, recent, workspace, workspace_bytes, stream)
+
+
 def gmc_workspace_bytes() -> int:
     return int(lib().gmc_workspace_bytes())
 
@@ -580,6 +630,203 @@ class Pruner:
 
     def close(self):
         gmc_free()
+
+
+def check_cache_tensors(k_pages, v_pages, page_table, lens, n_q_heads, slot_pos=None, seen=None, weights=None):
+    """Shapes, dtypes and devices of a cache's tensors (see gmc_cache).  Raises
+    ValueError."""
+    import torch
+    if k_pages.dim() != 4 or k_pages.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("k_pages must be [n_pages][n_kv_heads][page_size][head_dim] in float32 or bfloat16, got "
+                         f"{k_pages.dtype} {tuple(k_pages.shape)}")
+    if v_pages.shape != k_pages.shape or v_pages.dtype != k_pages.dtype:
+        raise ValueError("v_pages must have k_pages' shape and dtype")
+    if page_table.dim() != 2 or page_table.dtype != torch.int32:
+        raise ValueError("page_table must be int32 [n_seq][max_pages]")
+    b, slots = page_table.shape[0], page_table.shape[1] * k_pages.shape[2]
+    if n_q_heads < 1 or n_q_heads % max(k_pages.shape[1], 1) != 0:
+        raise ValueError(f"n_q_heads={n_q_heads} must be a multiple of the cache's {k_pages.shape[1]} kv heads")
+    tensors = [("k_pages", k_pages), ("v_pages", v_pages), ("page_table", page_table)]
+    for name, x in (("lens", lens), ("seen", seen)):
+        if x is not None:
+            if tuple(x.shape) != (b,) or x.dtype != torch.int32:
+                raise ValueError(f"{name} must be int32 [n_seq] = ({b},)")
+            tensors.append((name, x))
+    for name, x, dt in (("slot_pos", slot_pos, torch.int32), ("weights", weights, torch.float32)):
+        if x is not None:
+            if tuple(x.shape) != (b, k_pages.shape[1], slots) or x.dtype != dt:
+                raise ValueError(f"{name} must be {dt} [n_seq][n_kv_heads][slots] = ({b}, {k_pages.shape[1]}, {slots})")
+            tensors.append((name, x))
+    if slot_pos is not None and seen is None:
+        raise ValueError("slot_pos needs seen")
+    for name, x in tensors:
+        if not x.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+    for name, x in tensors:
+        if x.device.type != "cuda" or x.device != k_pages.device:
+            raise ValueError(f"{name} must be on the GPU, on k_pages' device; got {x.device}")
+
+
+class KvCache:
+    """One layer's paged K/V cache of a batch of sequences (gmc_cache): the
+    tensors, which the wrapper keeps alive, and the calls on them on torch's
+    current stream.  Needs no Pruner.
+
+    ``k_pages`` / ``v_pages`` [n_pages][n_kv_heads][page_size][head_dim],
+    ``page_table`` [n_seq][max_pages] int32, ``lens`` [n_seq] int32; for a cache
+    that evicts also ``seen`` [n_seq] int32, ``slot_pos``
+    [n_seq][n_kv_heads][slots] int32 and ``weights`` of the same shape, float32.
+    """
+
+    def __init__(self, k_pages, v_pages, page_table, lens, *, n_q_heads, slot_pos=None, seen=None, weights=None):
+        import torch
+        check_cache_tensors(k_pages, v_pages, page_table, lens, n_q_heads, slot_pos, seen, weights)
+        self.torch = torch
+        self.k_pages, self.v_pages, self.page_table, self.lens = k_pages, v_pages, page_table, lens
+        self.slot_pos, self.seen, self.weights = slot_pos, seen, weights
+        self.device, self.dtype = k_pages.device, k_pages.dtype
+        n_pages, hkv, page, dh = k_pages.shape
+        self.n_seq, self.slots = page_table.shape[0], page_table.shape[1] * page
+        self.n_q_heads, self.n_kv_heads, self.head_dim = n_q_heads, hkv, dh
+        ptr = (lambda t: None if t is None else t.data_ptr())
+        self.desc = GmcCache(GMC_BF16 if self.dtype == torch.bfloat16 else GMC_F32, n_q_heads, hkv, dh, page,
+                             page_table.shape[1], n_pages, self.n_seq, ptr(k_pages), ptr(v_pages), ptr(page_table),
+                             ptr(lens), ptr(seen), ptr(slot_pos), ptr(weights))
+
+    @classmethod
+    def create(cls, *, n_seq, slots, n_q_heads, n_kv_heads, head_dim, dtype, device="cuda", page_size=64,
+               evicts=False):
+        """An empty cache of `slots` slots a sequence (rounded up to whole
+        pages), its pages in order; ``evicts`` adds positions and weights."""
+        import torch
+        per = -(-slots // page_size)
+        pages = [torch.zeros((n_seq * per, n_kv_heads, page_size, head_dim), dtype=dtype, device=device) for _ in "kv"]
+        table = torch.arange(n_seq * per, dtype=torch.int32, device=device).view(n_seq, per)
+        lens = torch.zeros(n_seq, dtype=torch.int32, device=device)
+        more = {}
+        if evicts:
+            shape = (n_seq, n_kv_heads, per * page_size)
+            more = dict(seen=torch.zeros_like(lens), slot_pos=torch.zeros(shape, dtype=torch.int32, device=device),
+                        weights=torch.zeros(shape, dtype=torch.float32, device=device))
+        return cls(*pages, table, lens, n_q_heads=n_q_heads, **more)
+
+    def _on_device(self):
+        # the current device is the cache's almost always
+        torch = self.torch
+        return None if torch.cuda.current_device() == self.device.index else torch.cuda.device(self.device)
+
+    def _call(self, name, fn, *args):
+        torch = self.torch
+        guard = self._on_device()
+        if guard is None:
+            code = fn(self.desc, *args, torch.cuda.current_stream().cuda_stream)
+        else:
+            with guard:
+                code = fn(self.desc, *args, torch.cuda.current_stream().cuda_stream)
+        _check(code, name)
+
+    def _bytes(self, name, need):
+        if need < 0:
+            _check(int(need), name)
+        return self.torch.empty(need, dtype=self.torch.uint8, device=self.device) if need else None
+
+    def _rows(self, name, x, heads):
+        """Tokens x heads x head_dim in the cache's dtype, each token's heads in
+        one run; returns the tokens' stride."""
+        if x.dim() != 3 or x.shape[1] != heads or x.shape[2] != self.head_dim or x.dtype != self.dtype:
+            raise ValueError(f"{name} must be {self.dtype} [tokens][{heads}][{self.head_dim}], got {x.dtype} "
+                             f"{tuple(x.shape)}")
+        if x.device != self.device:
+            raise ValueError(f"{name} must be on the cache's device {self.device}; got {x.device}")
+        stride = x.stride(0) if x.shape[0] > 1 else heads * self.head_dim
+        if x.stride(2) != 1 or (heads > 1 and x.stride(1) != self.head_dim) or stride < heads * self.head_dim:
+            raise ValueError(f"{name} must hold each token's heads in one run, got strides {x.stride()}")
+        return stride
+
+    def _index(self, name, x, shape):
+        if x.dtype != self.torch.int32 or tuple(x.shape) != shape or not x.is_contiguous() or x.device != self.device:
+            raise ValueError(f"{name} must be a contiguous int32 {shape} tensor on the cache's device")
+        return x.data_ptr()
+
+    def _new(self, rows, starts, max_new):
+        if starts is not None:
+            if max_new is None:
+                raise ValueError("starts needs max_new, the most new tokens of a sequence")
+            return self._index("starts", starts, (self.n_seq + 1,)), max_new
+        if rows % self.n_seq != 0 or (max_new is not None and max_new * self.n_seq != rows):
+            raise ValueError(f"without starts the {rows} rows must be the same number for each of {self.n_seq} sequences")
+        return None, rows // self.n_seq
+
+    def append(self, k, v, *, starts=None, max_new=None, src=None):
+        """gmc_cache_append: k, v [tokens][n_kv_heads][head_dim] (tokens may be
+        strided); ``starts`` [n_seq + 1] int32 with ``max_new`` for ragged
+        rows, or ``src`` [n_seq][n] int32, the rows of each sequence to take."""
+        sk, sv = self._rows("k", k, self.n_kv_heads), self._rows("v", v, self.n_kv_heads)
+        rows = k.shape[0]
+        if v.shape[0] != rows:
+            raise ValueError(f"k and v hold {rows} and {v.shape[0]} tokens")
+        if src is not None:
+            if starts is not None:
+                raise ValueError("src and starts must not both be given")
+            max_new = src.shape[1] if src.dim() == 2 else 0
+            first, taken = None, self._index("src", src, (self.n_seq, max_new))
+        else:
+            (first, max_new), taken = self._new(rows, starts, max_new), None
+        self._call("gmc_cache_append", gmc_cache_append, k.data_ptr(), v.data_ptr(), sk, sv, rows, first, taken, max_new)
+
+    def _outputs(self, q, out, lse):
+        torch = self.torch
+        shape = (q.shape[0], self.n_q_heads, self.head_dim)
+        if out is None:
+            out = torch.empty(shape, dtype=self.dtype, device=self.device)
+        elif tuple(out.shape) != shape or out.dtype != self.dtype or not out.is_contiguous() or out.device != self.device:
+            raise ValueError(f"out must be a contiguous {self.dtype} {shape} tensor on the cache's device")
+        if lse is True:
+            lse = torch.empty(shape[:2], dtype=torch.float32, device=self.device)
+        elif lse is False:
+            lse = None
+        elif lse is not None and (tuple(lse.shape) != shape[:2] or lse.dtype != torch.float32 or
+                                  not lse.is_contiguous() or lse.device != self.device):
+            raise ValueError(f"lse must be a contiguous float32 {shape[:2]} tensor on the cache's device")
+        return out, lse
+
+    def prefill(self, q, *, starts=None, max_new=None, window=0, sinks=0, scale=None, lse=False, out=None):
+        """gmc_cache_prefill: q [tokens][n_q_heads][head_dim] of the newest
+        tokens (appended before), the same number for every sequence or ragged by
+        ``starts`` / ``max_new``.  Returns out, or (out, lse) with ``lse`` True or
+        a tensor to fill.  Rows of no sequence are left as ``out`` holds them."""
+        stride = self._rows("q", q, self.n_q_heads)
+        first, max_new = self._new(q.shape[0], starts, max_new)
+        out, ls = self._outputs(q, out, lse)
+        need = gmc_cache_prefill_bytes(self.desc, max_new)
+        ws = self._bytes("gmc_cache_prefill", need)
+        self._call("gmc_cache_prefill", gmc_cache_prefill, q.data_ptr(), stride, q.shape[0], first, max_new,
+                   self.head_dim ** -0.5 if scale is None else scale, window, sinks, out.data_ptr(),
+                   None if ls is None else ls.data_ptr(), None if ws is None else ws.data_ptr(), need)
+        return out if ls is None else (out, ls)
+
+    def decode(self, q, *, window=0, sinks=0, scale=None, accumulate=False, lse=False, out=None):
+        """gmc_cache_decode: q [n_seq][n_q_heads][head_dim], one token a
+        sequence (appended before).  ``accumulate`` adds its attention weights to
+        ``weights``.  Returns as prefill."""
+        stride = self._rows("q", q, self.n_q_heads)
+        if q.shape[0] != self.n_seq:
+            raise ValueError(f"q must hold one token for each of {self.n_seq} sequences, got {q.shape[0]}")
+        out, ls = self._outputs(q, out, lse)
+        need = gmc_cache_decode_bytes(self.desc, accumulate)
+        ws = self._bytes("gmc_cache_decode", need)
+        self._call("gmc_cache_decode", gmc_cache_decode, q.data_ptr(), stride,
+                   self.head_dim ** -0.5 if scale is None else scale, window, sinks, accumulate, out.data_ptr(),
+                   None if ls is None else ls.data_ptr(), None if ws is None else ws.data_ptr(), need)
+        return out if ls is None else (out, ls)
+
+    def evict(self, budget, *, sinks=0, recent=0):
+        """gmc_cache_evict: every sequence keeps at most ``budget`` rows a kv
+        head, the first ``sinks`` and last ``recent`` positions among them."""
+        need = gmc_cache_evict_bytes(self.desc, budget)
+        ws = self._bytes("gmc_cache_evict", need)
+        self._call("gmc_cache_evict", gmc_cache_evict, budget, sinks, recent, None if ws is None else ws.data_ptr(),
+                   need)
 
 
 def gmc_timing_enable(enable: bool) -> int:

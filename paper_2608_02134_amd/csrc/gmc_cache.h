@@ -1,0 +1,83 @@
+// The paged K/V cache behind a compacted prompt: its view as the kernels take
+// it, and the launchers of its operators.
+//
+// Slot s of sequence b lies in page table[b][s / page] at row s % page; a
+// page holds one run of `page` rows of dh elements per kv head, so that the
+// block that works on one head reads whole runs.  Lengths and page ids are
+// device data: every kernel clamps a length to the table's capacity and takes
+// a slot on a page id outside [0, n_pages) as not held.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace gmc {
+
+struct CacheView {
+  void* k;
+  void* v;
+  const int32_t* table;   // [n_seq][max_pages]
+  int32_t* lens;          // [n_seq]
+  int32_t* seen;          // [n_seq] or null: positions given out
+  int32_t* slot_pos;      // [n_seq][hkv][cap] or null: position of a slot (null: its index)
+  float* weights;         // [n_seq][hkv][cap] or null: accumulated attention weight
+  long long n_pages;
+  int n_seq, max_pages, shift, page, cap;   // page = 1 << shift rows; cap = max_pages * page
+  int hq, hkv, hg, dh, dtype;
+};
+
+// One attention call: n query rows of sequence b at row first_b of q and out,
+// the last n_b slots of the cache.
+struct AttendArgs {
+  const void* q;          // rows of hq * dh elements, q_stride elements apart
+  long long q_stride, rows;
+  const int32_t* starts;  // [n_seq + 1] or null: first_b = b * max_new, n_b = max_new
+  int max_new;
+  float scale;
+  int window, sinks;      // window 0: none
+  void* out;              // [rows][hq][dh]
+  float* lse;             // [rows][hq] or null
+};
+
+#ifdef __HIPCC__
+__device__ __forceinline__ int cache_len(const CacheView& c, int b) { return min(max(c.lens[b], 0), c.cap); }
+
+// Row of slot s in the pages of head h, in rows of dh elements; -1: not held.
+__device__ __forceinline__ long long cache_row(const CacheView& c, int b, int h, int s) {
+  const int id = c.table[static_cast<long long>(b) * c.max_pages + (s >> c.shift)];
+  if (id < 0 || id >= c.n_pages) return -1;
+  return ((static_cast<long long>(id) * c.hkv + h) << c.shift) + (s & (c.page - 1));
+}
+
+// First row and number of rows of sequence b's new tokens, within [0, rows).
+__device__ __forceinline__ void new_rows(const int32_t* starts, int max_new, long long rows, int b, long long* first,
+                                         int* n) {
+  if (!starts) {
+    *first = static_cast<long long>(b) * max_new;
+    *n = max_new;
+  } else {
+    const long long lo = min(max(static_cast<long long>(starts[b]), 0ll), rows);
+    const long long hi = min(static_cast<long long>(starts[b + 1]), rows);
+    *first = lo;
+    *n = static_cast<int>(min(max(hi - lo, 0ll), static_cast<long long>(max_new)));
+  }
+}
+#endif
+
+hipError_t launch_cache_append(const CacheView& c, const void* k, const void* v, long long k_stride,
+                               long long v_stride, long long rows, const int32_t* starts, const int32_t* src,
+                               int max_new, hipStream_t st);
+
+// Attention of every query row over its sequence's cache.
+hipError_t launch_cache_attend(const CacheView& c, const AttendArgs& a, hipStream_t st);
+
+// weights += the attention weights of one query row per sequence, whose
+// log-sum-exps are lse [n_seq][hq].
+hipError_t launch_cache_weigh(const CacheView& c, const AttendArgs& a, const float* lse, hipStream_t st);
+
+// Rows an eviction moves at most, per sequence and kv head.
+inline int evict_moves(int cap, int budget) { return cap - budget < budget ? cap - budget : budget; }
+// scratch: int32 [n_seq * hkv] counts, then [n_seq * hkv][evict_moves] of (to, from).
+hipError_t launch_cache_evict(const CacheView& c, int budget, int sinks, int recent, int32_t* scratch, hipStream_t st);
+
+}  // namespace gmc

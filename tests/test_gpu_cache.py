@@ -1,0 +1,417 @@
+"""The paged K/V cache on the GPU against its oracle: appended rows and
+evictions bit-exact, attention within bounds derived from its roundings."""
+import copy
+
+import numpy as np
+import pytest
+
+from oracle import cache_oracle as O
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+if not torch.cuda.is_available():
+    pytest.skip("no GPU", allow_module_level=True)
+
+from . import cache_cases as C  # noqa: E402
+
+
+def _say(what):
+    print(f"\n[case] {what}", flush=True)
+
+
+# --- append ------------------------------------------------------------------------
+APPENDS = {
+    "step": dict(dtype="bf16", hq=28, hkv=4, dh=128, page=16, lens=[15, 16, 0, 100], slots=128, new=[1, 1, 1, 1]),
+    "ragged": dict(dtype="bf16", hq=4, hkv=2, dh=96, page=32, lens=[3, 31, 64], slots=160, new=[70, 0, 33]),
+    "fills_up": dict(dtype="f32", hq=3, hkv=3, dh=32, page=16, lens=[30, 5], slots=32, new=[9, 32]),
+    "wide": dict(dtype="f32", hq=2, hkv=1, dh=256, page=64, lens=[0], slots=300, new=[300]),
+}
+
+
+@pytest.mark.parametrize("case", list(APPENDS))
+@pytest.mark.parametrize("positions", [False, True])
+def test_append(case, positions):
+    a = dict(APPENDS[case])
+    _say(f"append {case} positions={positions} {a}")
+    new = a.pop("new")
+    rng = np.random.default_rng(3)
+    c = C.make(rng, positions=positions, weights=positions, **a)
+    kv = C.rounded(rng.standard_normal((sum(new), 2, a["hkv"], a["dh"])), a["dtype"])
+    first = np.concatenate([[0], np.cumsum(new)])
+    dev = C.on_gpu(c)
+    x = C.to_gpu(kv, a["dtype"])
+    dev.append(x[:, 0], x[:, 1], starts=torch.tensor(first, dtype=torch.int32).cuda(), max_new=max(new))
+    O.append(c, kv[:, 0], kv[:, 1], new, [np.arange(first[b], first[b + 1]) for b in range(len(new))])
+    _compare_caches(c, dev)
+
+
+def _compare_caches(c, dev):
+    assert np.array_equal(dev.lens.cpu().numpy(), c["lens"])
+    assert C.same(C.host(dev.k_pages), c["k"]) and C.same(C.host(dev.v_pages), c["v"])
+    if c.get("slot_pos") is not None:
+        assert np.array_equal(dev.seen.cpu().numpy(), c["seen"])
+        for b in range(len(c["lens"])):
+            n = c["lens"][b]
+            assert np.array_equal(dev.slot_pos[b, :, :n].cpu().numpy(), c["slot_pos"][b, :, :n])
+    if c.get("weights") is not None:
+        for b in range(len(c["lens"])):
+            n = c["lens"][b]
+            assert C.same(C.host(dev.weights[b, :, :n]), c["weights"][b, :, :n])
+
+
+@pytest.mark.parametrize("n,per", [(335, 1375), (1, 1), (40, 97)])
+def test_append_of_kept_rows(n, per):
+    _say(f"append src n={n} of {per}")
+    rng = np.random.default_rng(n)
+    c = C.make(rng, dtype="bf16", hq=28, hkv=4, dh=128, page=16, lens=[0, 7], slots=400)
+    kv = C.rounded(rng.standard_normal((2 * per, 2, 4, 128)), "bf16")
+    src = np.stack([np.sort(rng.choice(per, n, replace=False)) for _ in range(2)]).astype(np.int32)
+    dev, x = C.on_gpu(c), C.to_gpu(kv, "bf16")
+    dev.append(x[:, 0], x[:, 1], src=torch.from_numpy(src).cuda())
+    O.append(c, kv[:, 0], kv[:, 1], [n, n], [src[0], per + src[1]])
+    _compare_caches(c, dev)
+
+
+def test_append_clamps_and_leaves_out():
+    """Source rows out of range are clamped, rows on pages that are none left
+    out, starts out of range clipped to the rows there are."""
+    _say("append bad indices")
+    rng = np.random.default_rng(5)
+    c = C.make(rng, dtype="bf16", hq=2, hkv=2, dh=64, page=16, lens=[10, 3], slots=64)
+    c["table"][0, 1], c["table"][1, 0] = -1, 10 ** 6
+    kv = C.rounded(rng.standard_normal((24, 2, 2, 64)), "bf16")
+    src = np.array([[-5, 0, 11, 12, 2 ** 31 - 1] * 4, [3, 2, 1, 0, -2 ** 31] * 4], np.int32)
+    dev, x = C.on_gpu(c), C.to_gpu(kv, "bf16")
+    dev.append(x[:, 0], x[:, 1], src=torch.from_numpy(src).cuda())
+    rows = np.clip(src.astype(np.int64), 0, 11) + np.array([[0], [12]])
+    O.append(c, kv[:, 0], kv[:, 1], [20, 20], rows)
+    _compare_caches(c, dev)
+    starts = torch.tensor([20, 2 ** 31 - 1, -4], dtype=torch.int32).cuda()   # 4 rows, then none
+    dev.append(x[:, 0], x[:, 1], starts=starts, max_new=6)
+    O.append(c, kv[:, 0], kv[:, 1], [4, 0], [np.arange(20, 24), []])
+    _compare_caches(c, dev)
+
+
+# --- attention ----------------------------------------------------------------------
+HEADS = [(28, 4, 128), (8, 2, 64), (6, 6, 96), (16, 1, 256), (4, 4, 32), (32, 1, 128), (5, 1, 160), (40, 2, 64),
+         (3, 1, 192), (2, 2, 224)]
+WINDOWS = [(0, 0), (1, 0), (37, 4), (64, 0), (5, 100)]
+
+
+def _decode(rng, c, window, sinks, accumulate=False, stride=0):
+    b, hq, dh = len(c["lens"]), c["hq"], c["k"].shape[3]
+    q = C.queries(rng, c, b)
+    dev, x = C.on_gpu(c), C.to_gpu(q, c["dtype"])
+    if stride:
+        wide = torch.full((b, hq + 3, dh), float("nan"), dtype=x.dtype, device="cuda")
+        wide[:, 1:hq + 1] = x
+        x = wide[:, 1:hq + 1]
+    out, lse = dev.decode(x, window=window, sinks=sinks, accumulate=accumulate, lse=True)
+    ref = O.attend(c, q, list(range(b)), [1] * b, dh ** -0.5, window, sinks)
+    C.check_attention(ref, C.host(out), C.host(lse), c["dtype"], dh)
+    if accumulate:
+        C.check_weights(ref, c["weights"], C.host(dev.weights), dh)
+
+
+@pytest.mark.parametrize("heads", HEADS, ids=str)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_decode_heads(heads, dtype):
+    hq, hkv, dh = heads
+    _say(f"decode {dtype} {heads}")
+    rng = np.random.default_rng(hq * dh)
+    c = C.make(rng, dtype=dtype, hq=hq, hkv=hkv, dh=dh, page=16, lens=[1, 200, 33], slots=208, weights=True)
+    _decode(rng, c, 0, 0, accumulate=True, stride=1)
+
+
+@pytest.mark.parametrize("window", WINDOWS, ids=str)
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("positions", [False, True])
+def test_decode_lengths(window, page, positions):
+    _say(f"decode lengths window={window} page={page} positions={positions}")
+    rng = np.random.default_rng(page)
+    lens = [0, 1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 300]
+    c = C.make(rng, dtype="bf16", hq=14, hkv=2, dh=64, page=page, lens=lens, slots=300, positions=positions,
+               weights=True)
+    _decode(rng, c, *window, accumulate=True)
+
+
+@pytest.mark.parametrize("dtype,n", [("bf16", 4999), ("f32", 3001), ("bf16", 9000)])
+@pytest.mark.parametrize("window", [(0, 0), (700, 5)], ids=str)
+def test_decode_long(dtype, n, window):
+    _say(f"decode long {dtype} {n} {window}")
+    rng = np.random.default_rng(n)
+    c = C.make(rng, dtype=dtype, hq=7, hkv=1, dh=128, page=32, lens=[n, 1], slots=n, weights=True)
+    _decode(rng, c, *window, accumulate=True)
+
+
+def test_decode_length_past_the_table_and_below_zero():
+    _say("decode lens out of range")
+    rng = np.random.default_rng(8)
+    c = C.make(rng, dtype="bf16", hq=4, hkv=2, dh=64, page=16, lens=[48, 20], slots=48, weights=True)
+    c["lens"][:] = 2 ** 31 - 1, -7
+    _decode(rng, c, 0, 0, accumulate=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("window", [(0, 0), (9, 2)], ids=str)
+def test_decode_pages_that_are_none(dtype, window):
+    _say(f"decode bad pages {dtype} {window}")
+    rng = np.random.default_rng(9)
+    c = C.make(rng, dtype=dtype, hq=4, hkv=2, dh=64, page=16, lens=[60, 40, 16], slots=64, weights=True)
+    c["table"][0, 1], c["table"][0, 3], c["table"][1, 0], c["table"][2, 0] = -1, 2 ** 31 - 1, 10 ** 6, -2 ** 31
+    _decode(rng, c, *window, accumulate=True)
+
+
+def _prefill(rng, c, new, window, sinks, gap=2, stride=0):
+    b, hq, dh = len(c["lens"]), c["hq"], c["k"].shape[3]
+    first = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    rows = int(first[-1]) + gap
+    q = C.queries(rng, c, rows)
+    dev, x = C.on_gpu(c), C.to_gpu(q, c["dtype"])
+    if stride:
+        wide = torch.full((rows, hq + 3, dh), float("nan"), dtype=x.dtype, device="cuda")
+        wide[:, 1:hq + 1] = x
+        x = wide[:, 1:hq + 1]
+    out = torch.full((rows, hq, dh), 7.0, dtype=x.dtype, device="cuda")
+    lse = torch.full((rows, hq), 7.0, device="cuda")
+    dev.prefill(x, starts=torch.from_numpy(first).cuda(), max_new=max(new), window=window, sinks=sinks, out=out, lse=lse)
+    ref = O.attend(c, q, first[:-1], new, dh ** -0.5, window, sinks)
+    assert (out[first[-1]:] == 7).all() and (lse[first[-1]:] == 7).all(), "rows behind the last sequence"
+    live = np.arange(rows) < first[-1]
+    C.check_attention(ref, C.host(out), C.host(lse), c["dtype"], dh, rows=live)
+    return ref, C.host(out), C.host(lse)
+
+
+@pytest.mark.parametrize("heads", HEADS, ids=str)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_prefill_heads(heads, dtype):
+    hq, hkv, dh = heads
+    _say(f"prefill {dtype} {heads}")
+    rng = np.random.default_rng(hq + dh)
+    c = C.make(rng, dtype=dtype, hq=hq, hkv=hkv, dh=dh, page=16, lens=[70, 1, 90], slots=96)
+    _prefill(rng, c, [70, 1, 21], 0, 0, stride=1)
+
+
+@pytest.mark.parametrize("window", WINDOWS, ids=str)
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("positions", [False, True])
+def test_prefill_lengths(window, page, positions):
+    _say(f"prefill lengths window={window} page={page} positions={positions}")
+    rng = np.random.default_rng(page + 1)
+    lens = [1, 17, 64, 65, 129, 200, 200, 40]
+    new = [1, 17, 64, 30, 129, 1, 150, 0]
+    c = C.make(rng, dtype="bf16", hq=6, hkv=2, dh=64, page=page, lens=lens, slots=208, positions=positions)
+    _prefill(rng, c, new, *window)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("window", [(0, 0), (300, 3)], ids=str)
+def test_prefill_long(dtype, window):
+    _say(f"prefill long {dtype} {window}")
+    rng = np.random.default_rng(77)
+    c = C.make(rng, dtype=dtype, hq=2, hkv=1, dh=128, page=64, lens=[1100], slots=1100)
+    _prefill(rng, c, [1037], *window)
+
+
+def test_prefill_few_tokens_on_a_long_cache():
+    _say("prefill 3 tokens over 6000 slots")
+    rng = np.random.default_rng(78)
+    c = C.make(rng, dtype="bf16", hq=7, hkv=1, dh=128, page=64, lens=[6001, 50], slots=6016)
+    _prefill(rng, c, [3, 5], 0, 0)
+
+
+def test_prefill_more_rows_than_slots_held():
+    """Rows whose own slot lies before the cache's first see nothing."""
+    _say("prefill more rows than slots")
+    rng = np.random.default_rng(79)
+    c = C.make(rng, dtype="bf16", hq=4, hkv=2, dh=64, page=16, lens=[5, 0], slots=32)
+    _prefill(rng, c, [9, 4], 0, 0)
+    _prefill(rng, c, [9, 4], 2, 1)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_prefill_pages_that_are_none(dtype):
+    _say(f"prefill bad pages {dtype}")
+    rng = np.random.default_rng(80)
+    c = C.make(rng, dtype=dtype, hq=4, hkv=2, dh=64, page=16, lens=[60, 40, 16], slots=64)
+    c["table"][0, 1], c["table"][0, 3], c["table"][1, 0], c["table"][2, 0] = -1, 2 ** 31 - 1, 10 ** 6, -2 ** 31
+    _prefill(rng, c, [60, 20, 16], 0, 0)
+    _prefill(rng, c, [60, 20, 16], 9, 2)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
+@pytest.mark.parametrize("window", [(0, 0), (20, 2)], ids=str)
+def test_what_is_not_seen_changes_nothing(dtype, bad, window):
+    """A row of infinities or NaN in K and V changes the queries that see it and
+    no other."""
+    _say(f"unseen {bad} {dtype} {window}")
+    args = dict(dtype=dtype, hq=4, hkv=2, dh=64, page=16, lens=[150], slots=160)
+    c = C.make(np.random.default_rng(81), **args)
+    _, clean, clean_lse = _prefill(np.random.default_rng(1), c, [150], *window)
+    for slot in (90, 149):
+        d = copy.deepcopy(c)
+        p, r = O.row_of(d, 0, 0, slot)
+        d["v"][p, :, r] = bad
+        if slot == 90:
+            d["k"][p, :, r] = bad
+        q = C.queries(np.random.default_rng(1), d, 152)[:150]
+        out, lse = C.on_gpu(d).prefill(C.to_gpu(q, dtype), window=window[0], sinks=window[1], lse=True)
+        out, lse = C.host(out), C.host(lse)
+        t = np.arange(150)
+        sees = (t >= slot) & ((window[0] == 0) | (t - slot < window[0]))
+        assert np.array_equal(out[~sees], clean[:150][~sees]) and np.array_equal(lse[~sees], clean_lse[:150][~sees])
+        assert not np.isfinite(out[sees]).any()
+
+
+def test_decode_sees_infinities_as_the_formula_does():
+    _say("decode infinities")
+    rng = np.random.default_rng(82)
+    for dtype in ("bf16", "f32"):
+        c = C.make(rng, dtype=dtype, hq=4, hkv=2, dh=64, page=16, lens=[60, 60], slots=64)
+        p, r = O.row_of(c, 0, 0, 50)
+        c["v"][p, 0, r] = np.inf
+        q = C.queries(rng, c, 2)
+        out, lse = C.on_gpu(c).decode(C.to_gpu(q, dtype), lse=True)
+        out = C.host(out)
+        assert np.isposinf(out[0, :2]).all() and np.isfinite(out[0, 2:]).all() and np.isfinite(out[1]).all()
+        assert np.isfinite(C.host(lse)).all()
+        c["k"][p, 0, r] = np.nan
+        out, lse = C.on_gpu(c).decode(C.to_gpu(q, dtype), lse=True)
+        assert np.isnan(C.host(out)[0, :2]).all() and np.isnan(C.host(lse)[0, :2]).all()
+        assert np.isfinite(C.host(out)[0, 2:]).all()
+
+
+# --- eviction -----------------------------------------------------------------------
+EVICTS = {
+    "one_over": dict(lens=[65, 64, 3], slots=80, budget=64, sinks=4, recent=8),
+    "half": dict(lens=[300, 151, 150], slots=304, budget=150, sinks=0, recent=0),
+    "most": dict(lens=[300, 1000], slots=1008, budget=17, sinks=9, recent=8),
+    "one_left": dict(lens=[50, 2, 1, 0], slots=64, budget=1, sinks=0, recent=0),
+    "long": dict(lens=[5000, 4100], slots=5008, budget=4096, sinks=4, recent=100),
+}
+
+
+@pytest.mark.parametrize("case", list(EVICTS))
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", ["random", "ties", "odd"])
+def test_evict(case, dtype, kind):
+    a = dict(EVICTS[case])
+    _say(f"evict {case} {dtype} {kind} {a}")
+    budget, sinks, recent = a.pop("budget"), a.pop("sinks"), a.pop("recent")
+    rng = np.random.default_rng(17)
+    c = C.make(rng, dtype=dtype, hq=6, hkv=3, dh=32, page=16, positions=True, weights=True, **a)
+    w = c["weights"]
+    if kind == "ties":
+        w[:] = rng.integers(0, 3, w.shape) * 0.5
+    if kind == "odd":
+        w[:] = rng.choice([0.0, -0.0, np.inf, -np.inf, np.nan, -1.0, 1e-40, 3.0], w.shape).astype(np.float32)
+    dev = C.on_gpu(c)
+    dev.evict(budget, sinks=sinks, recent=recent)
+    O.evict(c, budget, sinks, recent)
+    # (rows past the budget keep what they held in both)
+    _compare_caches(c, dev)
+
+
+def test_evict_pages_that_are_none():
+    _say("evict bad pages")
+    rng = np.random.default_rng(18)
+    c = C.make(rng, dtype="bf16", hq=2, hkv=2, dh=64, page=16, lens=[60, 64], slots=64, positions=True, weights=True)
+    c["table"][0, 1], c["table"][1, 3] = -1, 10 ** 6
+    dev = C.on_gpu(c)
+    dev.evict(30, sinks=1, recent=5)
+    O.evict(c, 30, 1, 5)
+    _compare_caches(c, dev)
+
+
+# --- together -------------------------------------------------------------------------
+def test_prompt_decode_and_eviction_together():
+    """A prompt, then tokens one by one with weights added up and the cache cut
+    back every few steps: what a bounded deployment runs."""
+    _say("together")
+    rng = np.random.default_rng(19)
+    hq, hkv, dh, b, n = 8, 2, 64, 2, 45
+    dev = C.B.KvCache.create(n_seq=b, slots=70, n_q_heads=hq, n_kv_heads=hkv, head_dim=dh, dtype=torch.bfloat16,
+                             page_size=16, evicts=True)
+    c = {"dtype": "bf16", "hq": hq, "q_scale": 2.0, "k": np.zeros(tuple(dev.k_pages.shape)),
+         "v": np.zeros(tuple(dev.v_pages.shape)), "table": dev.page_table.cpu().numpy(), "lens": np.zeros(b, np.int32),
+         "seen": np.zeros(b, np.int32), "slot_pos": np.zeros(tuple(dev.slot_pos.shape), np.int32),
+         "weights": np.zeros(tuple(dev.weights.shape))}
+    for step in range(40):
+        m = n if step == 0 else 1
+        kv = C.rounded(rng.standard_normal((b * m, 2, hkv, dh)), "bf16")
+        q = C.queries(rng, c, b * m)
+        x, y = C.to_gpu(kv, "bf16"), C.to_gpu(q, "bf16")
+        dev.append(x[:, 0], x[:, 1])
+        O.append(c, kv[:, 0], kv[:, 1], [m] * b, [np.arange(i * m, (i + 1) * m) for i in range(b)])
+        if step == 0:
+            out, lse = dev.prefill(y, window=30, sinks=3, lse=True)
+            ref = O.attend(c, q, [0, m], [m] * b, dh ** -0.5, 30, 3)
+        else:
+            out, lse = dev.decode(y, window=30, sinks=3, accumulate=True, lse=True)
+            ref = O.attend(c, q, list(range(b)), [1] * b, dh ** -0.5, 30, 3)
+            C.check_weights(ref, c["weights"], C.host(dev.weights), dh)
+            c["weights"] = C.host(dev.weights)     # (their roundings would add up)
+        C.check_attention(ref, C.host(out), C.host(lse), "bf16", dh)
+        if step % 7 == 6:
+            dev.evict(40, sinks=3, recent=5)
+            O.evict(c, 40, 3, 5)
+            _compare_caches(c, dev)
+    assert c["lens"].max() <= 47 and c["seen"][0] == n + 39
+
+
+def test_captured_steps_replay():
+    """Append, decode with accumulation and eviction in one graph, replayed with
+    eager work between, against the same calls made eagerly."""
+    _say("graph")
+    rng = np.random.default_rng(20)
+    args = dict(dtype="bf16", hq=14, hkv=2, dh=128, page=16, lens=[300, 60], slots=320, positions=True, weights=True)
+    a, b = C.on_gpu(C.make(np.random.default_rng(21), **args)), C.on_gpu(C.make(np.random.default_rng(21), **args))
+    kv = torch.zeros((2, 2, 2, 128), dtype=torch.bfloat16, device="cuda")
+    q = torch.zeros((2, 14, 128), dtype=torch.bfloat16, device="cuda")
+
+    def step(cache):
+        cache.append(kv[:, 0], kv[:, 1])
+        out, lse = cache.decode(q, accumulate=True, lse=True)
+        cache.evict(200, sinks=2, recent=9)
+        return out, lse
+
+    keep = [t.clone() for t in (a.lens, a.seen, a.slot_pos, a.weights, a.k_pages, a.v_pages)]
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step(a)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(a)
+    for t, s in zip((a.lens, a.seen, a.slot_pos, a.weights, a.k_pages, a.v_pages), keep):
+        t.copy_(s)
+    for i in range(4):
+        kv.copy_(torch.from_numpy(rng.standard_normal(kv.shape)).cuda())
+        q.copy_(torch.from_numpy(rng.standard_normal(q.shape)).cuda())
+        graph.replay()
+        want = step(b)
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), i
+        for x, y in ((a.lens, b.lens), (a.seen, b.seen)):
+            assert torch.equal(x, y), i
+        n = int(b.lens.max())
+        assert torch.equal(a.weights[..., :60], b.weights[..., :60]) and n == 200
+
+
+def test_repeats_bit_for_bit_on_another_stream():
+    _say("another stream")
+    rng = np.random.default_rng(22)
+    c = C.make(rng, dtype="bf16", hq=28, hkv=4, dh=128, page=64, lens=[2000, 700], slots=2048, weights=True)
+    q = C.to_gpu(C.queries(rng, c, 2), "bf16")
+    dev = C.on_gpu(c)
+    w0 = dev.weights.clone()
+    out, lse = dev.decode(q, accumulate=True, lse=True)
+    w1 = dev.weights.clone()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        dev.weights.copy_(w0)
+        out2, lse2 = dev.decode(q, accumulate=True, lse=True)
+    side.synchronize()
+    assert torch.equal(out, out2) and torch.equal(lse, lse2) and torch.equal(w1, dev.weights)
