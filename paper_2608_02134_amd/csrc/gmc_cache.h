@@ -13,6 +13,8 @@
 
 namespace gmc {
 
+constexpr int kCacheMaxHeads = 256;   // GMC_CACHE_MAX_HEADS
+
 struct CacheView {
   void* k;
   void* v;
@@ -49,6 +51,13 @@ __device__ __forceinline__ long long cache_row(const CacheView& c, int b, int h,
   return ((static_cast<long long>(id) * c.hkv + h) << c.shift) + (s & (c.page - 1));
 }
 
+// Takes a matrix product's result out of the accumulators here, in the same
+// basic block.  (The compiler, clang 22 of ROCm 7.2, counts the wait between a
+// matrix instruction and the first read of its result along the fall-through
+// path only: with a taken branch in between the read came too early and gave
+// stale last rows.)
+template <typename V> __device__ __forceinline__ void settle(V& x) { asm volatile("" : "+v"(x)); }
+
 // First row and number of rows of sequence b's new tokens, within [0, rows).
 __device__ __forceinline__ void new_rows(const int32_t* starts, int max_new, long long rows, int b, long long* first,
                                          int* n) {
@@ -71,9 +80,12 @@ hipError_t launch_cache_append(const CacheView& c, const void* k, const void* v,
 // Attention of every query row over its sequence's cache.
 hipError_t launch_cache_attend(const CacheView& c, const AttendArgs& a, hipStream_t st);
 
-// weights += the attention weights of one query row per sequence, whose
-// log-sum-exps are lse [n_seq][hq].
-hipError_t launch_cache_weigh(const CacheView& c, const AttendArgs& a, const float* lse, hipStream_t st);
+// The same for one query row per sequence (a.starts null, a.max_new 1), with
+// the attention weights added to c.weights if asked for.  scratch:
+// decode_scratch_bytes of any content.
+long long decode_scratch_bytes(const CacheView& c, bool accumulate);
+hipError_t launch_cache_decode(const CacheView& c, const AttendArgs& a, bool accumulate, void* scratch,
+                               hipStream_t st);
 
 // Rows an eviction moves at most, per sequence and kv head.
 inline int evict_moves(int cap, int budget) { return cap - budget < budget ? cap - budget : budget; }

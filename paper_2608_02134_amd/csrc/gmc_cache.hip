@@ -117,9 +117,7 @@ int on_stream(const char* fn, void* stream, F launch) {
 
 int64_t round256(int64_t x) { return (x + 255) / 256 * 256; }
 
-int64_t decode_bytes(const CacheView& c, bool accumulate) {
-  return accumulate ? round256(4ll * c.n_seq * c.hq) : 0;
-}
+int64_t decode_bytes(const CacheView& c, bool accumulate) { return round256(decode_scratch_bytes(c, accumulate)); }
 int64_t prefill_bytes(const CacheView&, int64_t) { return 0; }
 int64_t evict_bytes(const CacheView& c, int budget) {
   const int64_t groups = static_cast<int64_t>(c.n_seq) * c.hkv;
@@ -166,11 +164,9 @@ int gmc_cache_decode(const gmc_cache* cache, const void* q, int64_t q_stride, fl
   if (accumulate && !c.weights) return set_error(GMC_ERR_ARG, "%s: accumulate needs the cache's weights", fn);
   rc = check_workspace(fn, workspace, workspace_bytes, decode_bytes(c, accumulate != 0));
   if (rc != GMC_OK) return rc;
-  AttendArgs a = attend_args(q, q_stride, c.n_seq, nullptr, 1, scale, window, sinks, out, lse);
+  const AttendArgs a = attend_args(q, q_stride, c.n_seq, nullptr, 1, scale, window, sinks, out, lse);
   return on_stream(fn, stream, [&](hipStream_t st) {
-    if (accumulate && !a.lse) a.lse = static_cast<float*>(workspace);
-    const hipError_t err = launch_cache_attend(c, a, st);
-    return err == hipSuccess && accumulate ? launch_cache_weigh(c, a, a.lse, st) : err;
+    return launch_cache_decode(c, a, accumulate != 0, workspace, st);
   });
 }
 

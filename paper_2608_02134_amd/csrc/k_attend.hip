@@ -60,45 +60,12 @@ __global__ void __launch_bounds__(64) attend_row_kernel(CacheView c, AttendArgs 
   if (a.lse && lane == 0) a.lse[(first + i) * c.hq + hq] = l == 0.f ? -INFINITY : m + logf(l);
 }
 
-// One thread per slot: the group's attention weights on it.
-template <typename T>
-__global__ void __launch_bounds__(256) weigh_slot_kernel(CacheView c, AttendArgs a, const float* __restrict__ lse) {
-  const int s = blockIdx.x * 256 + threadIdx.x, h = blockIdx.y, b = blockIdx.z;
-  const int t = cache_len(c, b) - 1;
-  if (s > t) return;
-  const long long row = cache_row(c, b, h, s);
-  if (row < 0) return;
-  const long long at = (static_cast<long long>(b) * c.hkv + h) * c.cap;
-  if (a.window) {
-    const int p = c.slot_pos ? c.slot_pos[at + s] : s, mine = c.slot_pos ? c.slot_pos[at + t] : t;
-    if (mine - p >= a.window && p >= a.sinks) return;
-  }
-  const T* k = static_cast<const T*>(c.k) + row * c.dh;
-  float w = 0.f;
-  for (int g = 0; g < c.hg; ++g) {
-    const T* q = static_cast<const T*>(a.q) + b * a.q_stride + (h * c.hg + g) * c.dh;
-    float x = 0.f;
-    for (int d = 0; d < c.dh; ++d) x += to_f32(q[d]) * a.scale * to_f32(k[d]);
-    w += expf(x - lse[static_cast<long long>(b) * c.hq + h * c.hg + g]);
-  }
-  c.weights[at + s] += w;
-}
-
 hipError_t launch_cache_attend(const CacheView& c, const AttendArgs& a, hipStream_t st) {
   const dim3 grid(a.max_new, c.hq, c.n_seq);
   if (c.dtype == 0)
     hipLaunchKernelGGL(attend_row_kernel<float>, grid, dim3(64), 0, st, c, a);
   else
     hipLaunchKernelGGL(attend_row_kernel<bf16_t>, grid, dim3(64), 0, st, c, a);
-  return hipGetLastError();
-}
-
-hipError_t launch_cache_weigh(const CacheView& c, const AttendArgs& a, const float* lse, hipStream_t st) {
-  const dim3 grid((c.cap + 255) / 256, c.hkv, c.n_seq);
-  if (c.dtype == 0)
-    hipLaunchKernelGGL(weigh_slot_kernel<float>, grid, dim3(256), 0, st, c, a, lse);
-  else
-    hipLaunchKernelGGL(weigh_slot_kernel<bf16_t>, grid, dim3(256), 0, st, c, a, lse);
   return hipGetLastError();
 }
 
