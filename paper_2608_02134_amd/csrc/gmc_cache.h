@@ -77,8 +77,10 @@ hipError_t launch_cache_append(const CacheView& c, const void* k, const void* v,
                                long long v_stride, long long rows, const int32_t* starts, const int32_t* src,
                                int max_new, hipStream_t st);
 
-// Attention of every query row over its sequence's cache.
-hipError_t launch_cache_attend(const CacheView& c, const AttendArgs& a, hipStream_t st);
+// Attention of every query row over its sequence's cache.  scratch:
+// prefill_scratch_bytes of any content.
+long long prefill_scratch_bytes(const CacheView& c, int max_new);
+hipError_t launch_cache_prefill(const CacheView& c, const AttendArgs& a, void* scratch, hipStream_t st);
 
 // The same for one query row per sequence (a.starts null, a.max_new 1), with
 // the attention weights added to c.weights if asked for.  scratch:

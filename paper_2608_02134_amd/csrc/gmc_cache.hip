@@ -118,7 +118,9 @@ int on_stream(const char* fn, void* stream, F launch) {
 int64_t round256(int64_t x) { return (x + 255) / 256 * 256; }
 
 int64_t decode_bytes(const CacheView& c, bool accumulate) { return round256(decode_scratch_bytes(c, accumulate)); }
-int64_t prefill_bytes(const CacheView&, int64_t) { return 0; }
+int64_t prefill_bytes(const CacheView& c, int64_t max_new) {
+  return round256(prefill_scratch_bytes(c, static_cast<int>(max_new)));
+}
 int64_t evict_bytes(const CacheView& c, int budget) {
   const int64_t groups = static_cast<int64_t>(c.n_seq) * c.hkv;
   return round256(4 * ((groups + 3) / 4 * 4) + 8 * groups * evict_moves(c.cap, budget));
@@ -188,9 +190,12 @@ int gmc_cache_prefill(const gmc_cache* cache, const void* q, int64_t q_stride, i
   if (rc != GMC_OK) return rc;
   if ((rc = check_attend(fn, c, q, q_stride, window, sinks, out)) != GMC_OK) return rc;
   if ((rc = check_new(fn, c, starts, max_new, rows)) != GMC_OK) return rc;
+  const int64_t row_blocks = (max_new * c.hg + 127) / 128;
+  if (row_blocks * c.hkv * c.n_seq > INT32_MAX)
+    return set_error(GMC_ERR_ARG, "%s: n_seq * max_new * n_q_heads above 2^38; split the call", fn);
   if ((rc = check_workspace(fn, workspace, workspace_bytes, prefill_bytes(c, max_new))) != GMC_OK) return rc;
   const AttendArgs a = attend_args(q, q_stride, rows, starts, max_new, scale, window, sinks, out, lse);
-  return on_stream(fn, stream, [&](hipStream_t st) { return launch_cache_attend(c, a, st); });
+  return on_stream(fn, stream, [&](hipStream_t st) { return launch_cache_prefill(c, a, workspace, st); });
 }
 
 int64_t gmc_cache_evict_bytes(const gmc_cache* cache, int64_t budget) {
