@@ -89,9 +89,8 @@ long long decode_scratch_bytes(const CacheView& c, bool accumulate);
 hipError_t launch_cache_decode(const CacheView& c, const AttendArgs& a, bool accumulate, void* scratch,
                                hipStream_t st);
 
-// Rows an eviction moves at most, per sequence and kv head.
-inline int evict_moves(int cap, int budget) { return cap - budget < budget ? cap - budget : budget; }
-// scratch: int32 [n_seq * hkv] counts, then [n_seq * hkv][evict_moves] of (to, from).
-hipError_t launch_cache_evict(const CacheView& c, int budget, int sinks, int recent, int32_t* scratch, hipStream_t st);
+// scratch: evict_scratch_bytes of any content.
+long long evict_scratch_bytes(const CacheView& c);
+hipError_t launch_cache_evict(const CacheView& c, int budget, int sinks, int recent, void* scratch, hipStream_t st);
 
 }  // namespace gmc

@@ -121,10 +121,7 @@ int64_t decode_bytes(const CacheView& c, bool accumulate) { return round256(deco
 int64_t prefill_bytes(const CacheView& c, int64_t max_new) {
   return round256(prefill_scratch_bytes(c, static_cast<int>(max_new)));
 }
-int64_t evict_bytes(const CacheView& c, int budget) {
-  const int64_t groups = static_cast<int64_t>(c.n_seq) * c.hkv;
-  return round256(4 * ((groups + 3) / 4 * 4) + 8 * groups * evict_moves(c.cap, budget));
-}
+int64_t evict_bytes(const CacheView& c) { return round256(evict_scratch_bytes(c)); }
 
 }  // namespace
 
@@ -203,7 +200,7 @@ int64_t gmc_cache_evict_bytes(const gmc_cache* cache, int64_t budget) {
   const int rc = check_cache("gmc_cache_evict_bytes", cache, &c);
   if (rc != GMC_OK) return rc;
   if (budget < 1) return set_error(GMC_ERR_ARG, "gmc_cache_evict_bytes: budget=%lld must be at least 1", ll(budget));
-  return budget >= c.cap ? 0 : evict_bytes(c, static_cast<int>(budget));
+  return budget >= c.cap ? 0 : evict_bytes(c);
 }
 
 int gmc_cache_evict(const gmc_cache* cache, int64_t budget, int64_t sinks, int64_t recent, void* workspace,
@@ -218,11 +215,11 @@ int gmc_cache_evict(const gmc_cache* cache, int64_t budget, int64_t sinks, int64
     return set_error(GMC_ERR_ARG, "%s: need budget >= 1 and sinks + recent <= budget, none negative (budget=%lld "
                      "sinks=%lld recent=%lld)", fn, ll(budget), ll(sinks), ll(recent));
   if (budget >= c.cap) return GMC_OK;   // no sequence can hold more
-  rc = check_workspace(fn, workspace, workspace_bytes, evict_bytes(c, static_cast<int>(budget)));
+  rc = check_workspace(fn, workspace, workspace_bytes, evict_bytes(c));
   if (rc != GMC_OK) return rc;
   return on_stream(fn, stream, [&](hipStream_t st) {
     return launch_cache_evict(c, static_cast<int>(budget), static_cast<int>(sinks), static_cast<int>(recent),
-                              static_cast<int32_t*>(workspace), st);
+                              workspace, st);
   });
 }
 

@@ -313,6 +313,25 @@ def test_evict(case, dtype, kind):
     _compare_caches(c, dev)
 
 
+@pytest.mark.parametrize("n,slots", [(8193, 8208), (30000, 65536), (66000, 66016)])
+@pytest.mark.parametrize("kind", ["random", "ties", "near"])
+def test_evict_long(n, slots, kind):
+    """Caches longer than one block keeps keys for; weights that agree in their
+    upper halves."""
+    _say(f"evict long {n} of {slots} {kind}")
+    rng = np.random.default_rng(n)
+    c = C.make(rng, dtype="bf16", hq=2, hkv=1, dh=32, page=16, lens=[n], slots=slots, positions=True, weights=True)
+    w = c["weights"]
+    if kind == "ties":
+        w[:] = np.where(rng.random(w.shape) < 0.7, 0.25, rng.random(w.shape).astype(np.float32))
+    if kind == "near":
+        w[:] = (1 + rng.integers(0, 1 << 15, w.shape) * 2.0 ** -23).astype(np.float32)
+    dev = C.on_gpu(c)
+    dev.evict(n // 3, sinks=4, recent=100)
+    O.evict(c, n // 3, 4, 100)
+    _compare_caches(c, dev)
+
+
 def test_evict_pages_that_are_none():
     _say("evict bad pages")
     rng = np.random.default_rng(18)
