@@ -187,8 +187,7 @@ int gmc_cache_prefill(const gmc_cache* cache, const void* q, int64_t q_stride, i
   if (rc != GMC_OK) return rc;
   if ((rc = check_attend(fn, c, q, q_stride, window, sinks, out)) != GMC_OK) return rc;
   if ((rc = check_new(fn, c, starts, max_new, rows)) != GMC_OK) return rc;
-  const int64_t row_blocks = (max_new * c.hg + 127) / 128;
-  if (row_blocks * c.hkv * c.n_seq > INT32_MAX)
+  if ((max_new * c.hg + 127) / 128 * c.hkv * c.n_seq > INT32_MAX)
     return set_error(GMC_ERR_ARG, "%s: n_seq * max_new * n_q_heads above 2^38; split the call", fn);
   if ((rc = check_workspace(fn, workspace, workspace_bytes, prefill_bytes(c, max_new))) != GMC_OK) return rc;
   const AttendArgs a = attend_args(q, q_stride, rows, starts, max_new, scale, window, sinks, out, lse);

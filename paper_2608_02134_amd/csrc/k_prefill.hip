@@ -29,6 +29,8 @@
 
 namespace gmc {
 
+// (the kernel's parts: out of line, what they share would live in memory)
+#define GMC_INLINE __attribute__((always_inline))
 constexpr int kPreWaves = 4, kPreRows = 32 * kPreWaves;
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef short shortx4 __attribute__((ext_vector_type(4)));
@@ -102,52 +104,44 @@ struct PreScratch {
   float* part;   // [n_seq * max_new][hq][nsplit][dh] unnormalised sums, or null
   float* ml;     // [n_seq * max_new][hq][nsplit][2] maximum (base 2) and sum
   int nsplit;
+  int run;       // blocks in a row that go to one XCD
 };
 // Splits that a block's tiles are shared over: none with fewer than two tiles.
 __device__ __forceinline__ int used_pre_splits(int tiles, int nsplit) { return min(nsplit, max(1, tiles / 2)); }
 
-template <typename T>
-__device__ __forceinline__ bool not_finite(uint32_t u) {
-  if constexpr (sizeof(T) == 4) return (u & 0x7F800000u) == 0x7F800000u;
-  return (u & 0x7F80u) == 0x7F80u || (u & 0x7F800000u) == 0x7F800000u;
-}
-
-// A value's bits: of kind 0 with infinities and NaN set to zero, of kind 1, 2
-// and 3 as 1 where it is +inf, -inf or NaN and 0 elsewhere.
-template <typename T>
-__device__ __forceinline__ uint32_t pick_special(uint32_t u, int kind) {
-  constexpr int S = sizeof(T) == 2 ? 16 : 0;
-  constexpr uint32_t kInf = 0x7F800000u >> S, kSign = 0x80000000u >> S, kOne = 0x3F800000u >> S;
-  const uint32_t mag = u & ~kSign;
-  if (kind == 0) return mag >= kInf ? 0u : u;
-  const bool hit = kind == 3 ? mag > kInf : u == (kind == 1 ? kInf : (kInf | kSign));
-  return hit ? kOne : 0u;
-}
-
 template <typename T, int DH>
 __global__ void __launch_bounds__(64 * kPreWaves, sizeof(T) == 2 && DH <= 128 ? 2 : 1)
-prefill_kernel(CacheView c, AttendArgs a, PreScratch sc, int row_blocks, int total) {
+prefill_kernel(CacheView c, AttendArgs a, PreScratch sc, int row_blocks) {
   using KTile = KeyTile<T, DH>;
   constexpr int CPR = KTile::CPR, KT = KTile::KT, KB = KT / 32, NB = DH / 32, PITCH = CPR * 16;
   constexpr int NS = sizeof(T) == 2 ? DH / 16 : DH / 8;    // reads of 16 bytes a lane needs of its K row
   constexpr int GROUPS = KT / 16;                          // runs of 16 slots, each on one page
   constexpr int LOADS = CPR / 4;                           // 1 KB loads of one run
-  __shared__ __align__(16) unsigned char k0[KT * PITCH], v0[KT * PITCH], k1[KT * PITCH], v1[KT * PITCH];
+  __shared__ __align__(16) unsigned char k_even[KT * PITCH], v_even[KT * PITCH], k_odd[KT * PITCH], v_odd[KT * PITCH];
+  __shared__ int special_seen;   // an infinity or NaN was taken out of a tile
 
-  // blocks of one XCD (every eighth) work on neighbouring tiles of the same
-  // heads, those with the most keys first
-  int id = blockIdx.x;
-  {
-    const int per = total / 8, more = total % 8, x = id % 8;
-    id = x * per + min(x, more) + id / 8;
-  }
-  const int split = id % sc.nsplit;
-  id /= sc.nsplit;
-  const int block = row_blocks - 1 - id % row_blocks, bh = id / row_blocks, h = bh % c.hkv, b = bh / c.hkv;
+  // Each of the eight XCDs (blocks go to them in turn) works on runs of
+  // neighbouring row blocks of a head, whose keys its L2 then holds, and the
+  // runs go round the XCDs, as sequences are of unlike lengths; in a head, rows
+  // with the most keys come first.
+  const int items = row_blocks * sc.nsplit, runs = (items + sc.run - 1) / sc.run;   // of a head
+  const int unit = (blockIdx.x / 8 / sc.run) * 8 + blockIdx.x % 8, bh = unit / runs;
+  const int item = (unit - bh * runs) * sc.run + blockIdx.x / 8 % sc.run;
+  if (bh >= c.hkv * c.n_seq || item >= items) return;
+  const int split = item % sc.nsplit, block = row_blocks - 1 - item / sc.nsplit, h = bh % c.hkv, b = bh / c.hkv;
   const PreWork wk = pre_work(c, a, b, block, KT);
   if (wk.rows <= 0) return;
   const int ns = used_pre_splits(wk.tiles, sc.nsplit);
-  if (split >= ns) return;
+  if (split >= ns) {   // no part: the join leaves it out
+    for (int x = threadIdx.x; x < wk.rows; x += 64 * kPreWaves) {
+      const int r = wk.row0 + x;
+      const long long part_row =
+          ((static_cast<long long>(b) * a.max_new + r / c.hg) * c.hq + h * c.hg + r % c.hg) * sc.nsplit + split;
+      sc.ml[2 * part_row] = -INFINITY;
+      sc.ml[2 * part_row + 1] = 0.f;
+    }
+    return;
+  }
   const int it0 = static_cast<int>(static_cast<long long>(wk.tiles) * split / ns);
   const int it1 = static_cast<int>(static_cast<long long>(wk.tiles) * (split + 1) / ns);
 
@@ -186,66 +180,73 @@ prefill_kernel(CacheView c, AttendArgs a, PreScratch sc, int row_blocks, int tot
   float m = -INFINITY, l = 0.f;
   const float slack = 8.f / cs;
 
-  // loads of one run of 16 slots: piece u of 64 chunks, by position in shared
-  // memory; the source chunk's byte offset in the run's rows
-  int src_off[LOADS];
-#pragma unroll
-  for (int u = 0; u < LOADS; ++u) {
+  // Offsets of a lane's reads.  With a power of two of chunks to a row they are
+  // exclusive ors of one offset each with constants, and are formed where they
+  // are used: kept, they took the registers that hold the running sums.
+  // Loads: piece u of a run of 16 slots, by position in shared memory; the source
+  // chunk's byte offset in the run's rows.
+  auto src_off = [&](int u) GMC_INLINE {
     const int p = 64 * u + lane, r = p / CPR;
-    src_off[u] = r * PITCH + KTile::chunk_at(r, p % CPR) * 16;
-  }
-  int k_off[NS];
-#pragma unroll
-  for (int s = 0; s < NS; ++s) k_off[s] = col * PITCH + KTile::place(col, 2 * s + half) * 16;
-  // bf16: two transposing reads of 4 keys x 16 dims; fp32: one value of a key
+    return r * PITCH + KTile::chunk_at(r, p % CPR) * 16;
+  };
+  constexpr bool kXor = KTile::kPow2;
   constexpr int VO = sizeof(T) == 2 ? 2 : 4;
-  int v_off[NB][VO];
+  int k_base[kXor ? 1 : NS], v_base[kXor ? 1 : NB][VO];
 #pragma unroll
-  for (int n = 0; n < NB; ++n)
+  for (int s = 0; s < (kXor ? 1 : NS); ++s) k_base[s] = col * PITCH + KTile::place(col, 2 * s + half) * 16;
+#pragma unroll
+  for (int n = 0; n < (kXor ? 1 : NB); ++n)
 #pragma unroll
     for (int e = 0; e < VO; ++e) {
-      if constexpr (sizeof(T) == 2) {
+      if constexpr (sizeof(T) == 2) {      // a transposing read of 4 keys x 16 dims
         const int i = lane & 15, r = 8 * e + 4 * half + (i >> 2);
         const int ch = 4 * n + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
-        v_off[n][e] = r * PITCH + KTile::place(r, ch) * 16 + 8 * (i & 1);
-      } else {
-        const int r = 4 * half + e;      // of 8 keys; the next 8 lie 8 rows on
-        v_off[n][e] = r * PITCH + KTile::place(r, 8 * n + (col >> 2)) * 16 + 4 * (col & 3);
+        v_base[n][e] = r * PITCH + KTile::place(r, ch) * 16 + 8 * (i & 1);
+      } else {                             // one value of a key
+        const int r = 4 * half + e;        // of 8 keys; the next 8 lie 8 rows on
+        v_base[n][e] = r * PITCH + KTile::place(r, 8 * n + (col >> 2)) * 16 + 4 * (col & 3);
       }
     }
+  auto k_off = [&](int s) GMC_INLINE { return kXor ? k_base[0] ^ (32 * s) : k_base[kXor ? 0 : s]; };
+  auto v_off = [&](int n, int e) GMC_INLINE {
+    return kXor ? v_base[0][e] ^ ((sizeof(T) == 2 ? 64 : 128) * n) : v_base[kXor ? 0 : n][e];
+  };
 
   const int32_t* table = c.table + static_cast<long long>(b) * c.max_pages;
   const long long page_bytes = static_cast<long long>(c.page) * PITCH;
+  auto slot0 = [&](int it) GMC_INLINE { return (it < wk.sink_tiles ? it : it + wk.skip) * KT; };
+  // The page ids of a tile's runs, one a lane (the first GROUPS lanes): fetched a
+  // tile before its loads start, which would wait for them (3900 of 7100 cycles
+  // a tile).
+  auto fetch = [&](int it) GMC_INLINE {
+    const int s = slot0(it) + 16 * (lane & (GROUPS - 1));
+    const int id = table[min(s, c.cap - 1) >> c.shift];
+    return it < it1 && s < wk.len ? id : -1;
+  };
   // Starts the loads of a tile; returns which of its runs are on a page.  A wave
   // loads K and V of one run (64 keys a tile), or one of the two (32 keys).
-  auto issue = [&](int it, shared_u8* ks, shared_u8* vs) -> unsigned {
-    const int s0 = (it < wk.sink_tiles ? it : it + wk.skip) * KT;
+  auto issue = [&](int it, int ids, shared_u8* ks, shared_u8* vs) GMC_INLINE -> unsigned {
+    const int s0 = slot0(it);
     constexpr bool kBoth = GROUPS == kPreWaves;
+    static_assert(kBoth || 2 * GROUPS == kPreWaves, "a wave loads K and V of a run, or one of them");
     const int mine = kBoth ? w : w >> 1;
-    unsigned ok = 0;
-    int pid = -1;
-#pragma unroll
-    for (int g = 0; g < GROUPS; ++g) {
-      const int s = s0 + 16 * g;
-      const int p = s < wk.len ? table[s >> c.shift] : -1;
-      const bool on = p >= 0 && p < c.n_pages;
-      ok |= on ? 1u << g : 0u;
-      pid = g == mine ? (on ? p : -1) : pid;
-    }
+    const bool on = ids >= 0 && ids < c.n_pages;
+    const unsigned ok = static_cast<unsigned>(__ballot(on)) & ((1u << GROUPS) - 1u);
+    const int pid = (ok >> mine) & 1u ? __builtin_amdgcn_readlane(ids, mine) : -1;
     const int s = s0 + 16 * mine, held = pid < 0 ? 0 : wk.len - s;   // rows of the run that are held
     const long long base =
         (static_cast<long long>(pid) * c.hkv + h) * page_bytes + static_cast<long long>(s & (c.page - 1)) * PITCH;
-    auto copy = [&](const void* pages, shared_u8* to) {
+    auto copy = [&](const void* pages, shared_u8* to) GMC_INLINE {
       const char* from = static_cast<const char*>(pages) + base;
       to += 16 * mine * PITCH;
       if (held >= 16) {
 #pragma unroll
         for (int u = 0; u < LOADS; ++u)
-          __builtin_amdgcn_global_load_lds((const global_u32*)(from + src_off[u]), to + 1024 * u, 16, 0, 0);
+          __builtin_amdgcn_global_load_lds((const global_u32*)(from + src_off(u)), to + 1024 * u, 16, 0, 0);
       } else {
 #pragma unroll
         for (int u = 0; u < LOADS; ++u) {
-          const char* at = (64 * u + lane) / CPR < held ? from + src_off[u] : reinterpret_cast<const char*>(kZeroRow);
+          const char* at = (64 * u + lane) / CPR < held ? from + src_off(u) : reinterpret_cast<const char*>(kZeroRow);
           __builtin_amdgcn_global_load_lds((const global_u32*)at, to + 1024 * u, 16, 0, 0);
         }
       }
@@ -259,41 +260,87 @@ prefill_kernel(CacheView c, AttendArgs a, PreScratch sc, int row_blocks, int tot
     return ok;
   };
 
-  auto compute = [&](int it, unsigned ok, const shared_u8* ks, const shared_u8* vs) {
-    const int s0 = (it < wk.sink_tiles ? it : it + wk.skip) * KT;
-    // some query of the block does not see some key of the tile
-    const bool block_edge = ok != (1u << GROUPS) - 1u || s0 + KT - 1 > wk.t_min || pos ||
-                            (a.window && wk.t_max - s0 >= a.window);
-    // then an infinity or NaN among the values must not reach that query
-    bool careful = false;
-    if (block_edge) {
-      uint32_t bad = 0;
-      for (int x = threadIdx.x; x < KT * CPR; x += 64 * kPreWaves) {
-        const u32x4 y = ld_shared<u32x4>(vs + 16 * x);
-        bad |= not_finite<T>(y.x) || not_finite<T>(y.y) || not_finite<T>(y.z) || not_finite<T>(y.w);
-      }
-      careful = __syncthreads_or(bad);
+  // Sets the infinities and NaN among a lane's 16 bytes of values to zero; returns
+  // whether there were any.
+  auto clean = [](u32x4& y) GMC_INLINE {
+    constexpr uint32_t kExp = sizeof(T) == 2 ? 0x7F807F80u : 0x7F800000u, kOne = sizeof(T) == 2 ? 0x00800080u : 0x00800000u;
+    constexpr uint32_t kTop = sizeof(T) == 2 ? 0x80008000u : 0x80000000u;
+    const uint32_t hit = (((y.x & kExp) + kOne) | ((y.y & kExp) + kOne) | ((y.z & kExp) + kOne) | ((y.w & kExp) + kOne)) & kTop;
+    if (!hit) return false;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t top = ((y[e] & kExp) + kOne) & kTop;   // a bit for each value that goes
+      y[e] = sizeof(T) == 2 ? y[e] & ~((top >> 15) * 0xFFFFu) : (top ? 0u : y[e]);
     }
-    if (s0 > wt_max) return;
-    const bool edge = ok != (1u << GROUPS) - 1u || s0 + KT - 1 > wt_min || pos || (a.window && wt_max - s0 >= a.window);
+    return true;
+  };
+  // whether some query of the block does not see some key of the tile
+  auto edge_of_block = [&](int s0, unsigned ok) GMC_INLINE {
+    return ok != (1u << GROUPS) - 1u || s0 + KT - 1 > wk.t_min || pos || (a.window && wk.t_max - s0 >= a.window);
+  };
+  // One tile; `inner`: every query of the block sees every key of it.  In another,
+  // an infinity or NaN among the values must not reach a query that does not see
+  // it, through a weight of zero: it is taken out here and added at the end.
+  auto compute = [&](auto inner, int it, unsigned ok, shared_u8* ks, shared_u8* vs) GMC_INLINE {
+    constexpr bool kInner = decltype(inner)::value;
+    const int s0 = slot0(it);
+    bool edge = false;
+    if constexpr (!kInner) {
+#pragma unroll
+      for (int x = 0; x < KT * CPR / (64 * kPreWaves); ++x) {
+        shared_u8* at = vs + 16 * (64 * kPreWaves * x + static_cast<int>(threadIdx.x));
+        u32x4 y = ld_shared<u32x4>(at);
+        if (clean(y)) {
+          *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(at) = y;
+          special_seen = 1;
+        }
+      }
+      __syncthreads();
+      if (s0 > wt_max) return;
+      edge = ok != (1u << GROUPS) - 1u || s0 + KT - 1 > wt_min || pos || (a.window && wt_max - s0 >= a.window);
+    }
 
+    if constexpr (kXor) {
+      asm volatile("" : "+v"(k_base[0]));   // (formed in each tile anew)
+#pragma unroll
+      for (int e = 0; e < VO; ++e) asm volatile("" : "+v"(v_base[0][e]));
+    }
     floatx16 x[KB];
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
+    for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
       for (int i = 0; i < 16; ++i) x[kb][i] = 0.f;
+    typedef __attribute__((address_space(3))) shortx4 shared4;
+    if constexpr (sizeof(T) == 2) {
+      // kAhead steps of K's reads before the first product, then one step of
+      // products for one of reads
+      constexpr int kAhead = NS < 4 ? NS : 4;
+      u32x4 kf[NS][KB];
+#pragma unroll
+      for (int s = 0; s < NS; ++s)
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) kf[s][kb] = ld_shared<u32x4>(ks + k_off(s) + 32 * kb * PITCH);
+#pragma unroll
+      for (int s = 0; s < NS; ++s)
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+          x[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[s][kb]),
+                                                          __builtin_bit_cast(bf16x8, q[s]), x[kb], 0, 0, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, kAhead * KB, 0);
+#pragma unroll
+      for (int s = 0; s < NS - kAhead; ++s) {
+        __builtin_amdgcn_sched_group_barrier(0x8, KB, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, KB, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x8, kAhead * KB, 0);
+    } else {
 #pragma unroll
       for (int s = 0; s < NS; ++s) {
-        const u32x4 kf = ld_shared<u32x4>(ks + k_off[s] + 32 * kb * PITCH);
-        if constexpr (sizeof(T) == 2) {
-          x[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf),
-                                                          __builtin_bit_cast(bf16x8, q[s]), x[kb], 0, 0, 0);
-        } else {
-          const uint32_t qe[4] = {q[s].x, q[s].y, q[s].z, q[s].w};
+        const u32x4 kf = ld_shared<u32x4>(ks + k_off(s));
+        const uint32_t qe[4] = {q[s].x, q[s].y, q[s].z, q[s].w};
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            x[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[e]), __uint_as_float(qe[e]), x[kb], 0, 0, 0);
-        }
+        for (int e = 0; e < 4; ++e)
+          x[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[e]), __uint_as_float(qe[e]), x[0], 0, 0, 0);
       }
     }
 #pragma unroll
@@ -338,94 +385,115 @@ prefill_kernel(CacheView c, AttendArgs a, PreScratch sc, int row_blocks, int tot
     }
     const float base = m == -INFINITY ? 0.f : m * cs;
     float sum = 0.f;
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float y = x[kb][i];
-        x[kb][i] = __builtin_amdgcn_exp2f(fmaf(y, cs, -base));
-        sum += x[kb][i];
-        // (a seen weight must not round to the zero of one that is not seen)
-        if (careful && y != -INFINITY) x[kb][i] = fmaxf(x[kb][i], 0x1p-126f) + 0.f * x[kb][i];
-      }
-    l += sum;
-    // kind 0: the product with the values (careful: those that are finite); 1 to
-    // 3: which sums contain a seen +inf, -inf or NaN
-    auto product = [&](auto clean, int kind, floatx16& acc, int n) {
-      if constexpr (sizeof(T) == 2) {
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-          for (int st = 0; st < 2; ++st) {
-            bf16x8 p;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) p[j] = static_cast<__bf16>(x[kb][8 * st + j]);
-            typedef __attribute__((address_space(3))) shortx4 shared4;
-            const shared_u8* vr = vs + (32 * kb + 16 * st) * PITCH;
-            const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((shared4*)(vr + v_off[n][0]));
-            const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((shared4*)(vr + v_off[n][1]));
-            auto both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-            if constexpr (decltype(clean)::value) {
-#pragma unroll
-              for (int j = 0; j < 8; ++j) both[j] = static_cast<short>(pick_special<T>(static_cast<uint16_t>(both[j]), kind));
-            }
-            acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, both), p, acc, 0, 0, 0);
-          }
-      } else {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          uint32_t v = ld_shared<uint32_t>(vs + 8 * (i >> 2) * PITCH + v_off[n][i & 3]);
-          if constexpr (decltype(clean)::value) v = pick_special<T>(v, kind);
-          acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(v), x[0][i], acc, 0, 0, 0);
-        }
-      }
+    // weight i of the lane's keys
+    auto weight = [&](int kb, int i) GMC_INLINE {
+      x[kb][i] = __builtin_amdgcn_exp2f(fmaf(x[kb][i], cs, -base));
+      sum += x[kb][i];
     };
-    if (careful) {
+    if constexpr (sizeof(T) == 2) {
+      // 16 keys at a time: their products are spread over the exponentials of
+      // the next 16 keys, whose values are read meanwhile
+      shortx4 v[2][NB][2];
+      auto read_values = [&](int st) GMC_INLINE {
 #pragma unroll
-      for (int n = 0; n < NB; ++n) product(std::true_type{}, 0, o[n], n);
-#pragma unroll 1
-      for (int kind = 1; kind < 4; ++kind) {
-        const float special = kind == 1 ? INFINITY : kind == 2 ? -INFINITY : NAN;
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            v[st % 2][n][e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((shared4*)(vs + 16 * st * PITCH + v_off(n, e)));
+      };
+      bf16x8 p[2];
+      auto weights = [&](int st) GMC_INLINE {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          weight(st / 2, 8 * (st % 2) + j);
+          p[st % 2][j] = static_cast<__bf16>(x[st / 2][8 * (st % 2) + j]);
+        }
+      };
+      read_values(0);
+      weights(0);
+#pragma unroll
+      for (int st = 0; st < 2 * KB; ++st) {
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
-          floatx16 acc;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) acc[i] = 0.f;
-          product(std::true_type{}, kind, acc, n);
-          settle(acc);
-#pragma unroll
-          for (int i = 0; i < 16; ++i) o[n][i] += acc[i] > 0.f ? special : 0.f;
+          const auto both = __builtin_shufflevector(v[st % 2][n][0], v[st % 2][n][1], 0, 1, 2, 3, 4, 5, 6, 7);
+          o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, both), p[st % 2], o[n], 0, 0, 0);
+        }
+        if (st + 1 < 2 * KB) {
+          read_values(st + 1);
+          weights(st + 1);
         }
       }
-      return;
-    }
+      l += sum;
+    } else {
 #pragma unroll
-    for (int n = 0; n < NB; ++n) product(std::false_type{}, 0, o[n], n);
+      for (int i = 0; i < 16; ++i) weight(0, i);
+      l += sum;
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+          o[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(ld_shared<float>(vs + 8 * (i >> 2) * PITCH + v_off(n, i & 3)), x[0][i],
+                                                      o[n], 0, 0, 0);
+    }
+  };
+  auto step = [&](int it, unsigned ok, shared_u8* ks, shared_u8* vs) GMC_INLINE {
+    if (edge_of_block(slot0(it), ok))
+      compute(std::false_type{}, it, ok, ks, vs);
+    else
+      compute(std::true_type{}, it, ok, ks, vs);
   };
   // a tile is in shared memory for all waves once each has waited for its loads
-  auto arrive = [&] {
+  auto arrive = [&]() GMC_INLINE {
     __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
     __syncthreads();
   };
 
-  shared_u8* const kb0 = (shared_u8*)k0;
-  shared_u8* const vb0 = (shared_u8*)v0;
-  shared_u8* const kb1 = (shared_u8*)k1;
-  shared_u8* const vb1 = (shared_u8*)v1;
+  shared_u8* const kb0 = (shared_u8*)k_even;
+  shared_u8* const vb0 = (shared_u8*)v_even;
+  shared_u8* const kb1 = (shared_u8*)k_odd;
+  shared_u8* const vb1 = (shared_u8*)v_odd;
+  if (threadIdx.x == 0) special_seen = 0;   // (seen after the first arrival)
   unsigned ok0 = 0, ok1 = 0;
-  if (it0 < it1) ok0 = issue(it0, kb0, vb0);
+  int ids = fetch(it0);
+  if (it0 < it1) ok0 = issue(it0, ids, kb0, vb0);
+  ids = fetch(it0 + 1);
   for (int it = it0; it < it1; it += 2) {
     arrive();
-    if (it + 1 < it1) ok1 = issue(it + 1, kb1, vb1);
-    compute(it, ok0, kb0, vb0);
+    if (it + 1 < it1) ok1 = issue(it + 1, ids, kb1, vb1);
+    ids = fetch(it + 2);
+    step(it, ok0, kb0, vb0);
     if (it + 1 >= it1) break;
     arrive();
-    if (it + 2 < it1) ok0 = issue(it + 2, kb0, vb0);
-    compute(it + 1, ok1, kb1, vb1);
+    if (it + 2 < it1) ok0 = issue(it + 2, ids, kb0, vb0);
+    ids = fetch(it + 3);
+    step(it + 1, ok1, kb1, vb1);
   }
-
   asm volatile("s_nop 15\n\ts_nop 7" ::: "memory");   // (see settle)
   __builtin_amdgcn_sched_barrier(0);
+  __syncthreads();
+  if (special_seen) {
+    // the infinities and NaN that were taken out, to the queries that see them
+#pragma unroll 1
+    for (int it = it0; it < it1; ++it) {
+      const unsigned ok = static_cast<unsigned>(__ballot(fetch(it) >= 0 && fetch(it) < c.n_pages)) & ((1u << GROUPS) - 1u);
+      if (!edge_of_block(slot0(it), ok)) continue;
+#pragma unroll 1
+      for (int s = slot0(it); s < min(slot0(it) + KT, wk.len); ++s) {
+        const long long row_at = cache_row(c, b, h, s);
+        if (row_at < 0) continue;
+        const int p = pos ? pos[s] : s;
+        const bool see = s <= t && (!a.window || mine - p < a.window || p < a.sinks);
+        const T* vp = static_cast<const T*>(c.v) + row_at * DH + 4 * half;
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const float v = to_f32<T>(vp[32 * n + 8 * (i >> 2) + (i & 3)]);
+            o[n][i] += see && !(fabsf(v) < INFINITY) ? v : 0.f;
+          }
+      }
+    }
+  }
   l = add_xor32(l);
   if (!live) return;
   const long long out_row = (wk.first + tok) * c.hq + hq;
@@ -467,38 +535,54 @@ prefill_kernel(CacheView c, AttendArgs a, PreScratch sc, int row_blocks, int tot
   if (a.lse && half == 0) a.lse[out_row] = l == 0.f ? -INFINITY : (mc + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
-// Joins the splits: one wave per row and head.
+// Joins the splits: one wave per row and head, four elements a lane.
 template <typename T>
 __global__ void __launch_bounds__(256)
-prefill_join_kernel(CacheView c, AttendArgs a, PreScratch sc, int kt) {
+prefill_join_kernel(CacheView c, AttendArgs a, PreScratch sc) {
   const int b = blockIdx.z, hq = blockIdx.y, i = blockIdx.x * 4 + wave_id(), lane = threadIdx.x & 63;
   long long first;
   int n;
   new_rows(a.starts, a.max_new, a.rows, b, &first, &n);
   if (i >= n) return;
-  const PreWork wk = pre_work(c, a, b, (i * c.hg + hq % c.hg) / kPreRows, kt);
-  const int ns = used_pre_splits(wk.tiles, sc.nsplit);
   const long long row = (first + i) * c.hq + hq, part_row = (static_cast<long long>(b) * a.max_new + i) * c.hq + hq;
   const float* ml = sc.ml + part_row * sc.nsplit * 2;
-  float m = -INFINITY;
-  for (int s = lane; s < ns; s += 64) m = fmaxf(m, ml[2 * s]);
-  m = wave_max(m);
-  const float base = m == -INFINITY ? 0.f : m;
-  float l = 0.f;
-  for (int s = lane; s < ns; s += 64) l += ml[2 * s + 1] * __builtin_amdgcn_exp2f(ml[2 * s] - base);
-  l = wave_sum(l);
-  float o[4] = {0.f, 0.f, 0.f, 0.f};
-  const float* part = sc.part + part_row * sc.nsplit * c.dh;
-  for (int s = 0; s < ns; ++s) {
-    const float f = __builtin_amdgcn_exp2f(ml[2 * s] - base);
+  const float* part = sc.part + part_row * sc.nsplit * c.dh + 4 * lane;
+  const bool mine = 4 * lane < c.dh;
+  constexpr int kFlight = 8;
+  float m = -INFINITY, l = 0.f;
+  floatx4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int s0 = 0; s0 < sc.nsplit; s0 += kFlight) {
+    floatx4 x[kFlight];
+    float mi[kFlight], li[kFlight];
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (lane + 64 * e < c.dh) o[e] += f * part[static_cast<long long>(s) * c.dh + lane + 64 * e];
+    for (int e = 0; e < kFlight; ++e) {
+      const int s = min(s0 + e, sc.nsplit - 1);
+      mi[e] = s0 + e < sc.nsplit ? ml[2 * s] : -INFINITY;
+      li[e] = s0 + e < sc.nsplit ? ml[2 * s + 1] : 0.f;
+      x[e] = floatx4{0.f, 0.f, 0.f, 0.f};
+      if (mine && (mi[e] != -INFINITY || li[e] != 0.f)) x[e] = *reinterpret_cast<const floatx4*>(part + static_cast<long long>(s) * c.dh);
+    }
+    float mn = m;
+#pragma unroll
+    for (int e = 0; e < kFlight; ++e) mn = fmaxf(mn, mi[e]);
+    const float base = mn == -INFINITY ? 0.f : mn, f = __builtin_amdgcn_exp2f(m - base);
+    l *= f;
+    o *= f;
+#pragma unroll
+    for (int e = 0; e < kFlight; ++e) {
+      const float g = __builtin_amdgcn_exp2f(mi[e] - base);
+      l += li[e] * g;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) o[u] += x[e][u] * g;
+    }
+    m = mn;
   }
+  if (mine) {
+    T* to = static_cast<T*>(a.out) + row * c.dh + 4 * lane;
+    const float inv = 1.f / l;
 #pragma unroll
-  for (int e = 0; e < 4; ++e)
-    if (lane + 64 * e < c.dh)
-      static_cast<T*>(a.out)[row * c.dh + lane + 64 * e] = from_f32<T>(l == 0.f ? 0.f : o[e] / l);
+    for (int u = 0; u < 4; ++u) to[u] = from_f32<T>(l == 0.f ? 0.f : o[u] * inv);
+  }
   if (a.lse && lane == 0)
     a.lse[row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
@@ -511,8 +595,8 @@ static int pre_row_blocks(const CacheView& c, int max_new) {
   return static_cast<int>((static_cast<long long>(max_new) * c.hg + kPreRows - 1) / kPreRows);
 }
 static int pre_splits(const CacheView& c, int max_new) {
-  const long long blocks = static_cast<long long>(pre_row_blocks(c, max_new)) * c.hkv * c.n_seq;
   const long long most = std::max(1, c.cap / pre_key_tile(c) / 2);
+  const long long blocks = static_cast<long long>(pre_row_blocks(c, max_new)) * c.hkv * c.n_seq;
   return static_cast<int>(std::max<long long>(1, std::min<long long>(most, 512 / blocks)));
 }
 
@@ -522,25 +606,27 @@ long long prefill_scratch_bytes(const CacheView& c, int max_new) {
 }
 
 hipError_t launch_cache_prefill(const CacheView& c, const AttendArgs& a, void* scratch, hipStream_t st) {
-  const int row_blocks = pre_row_blocks(c, a.max_new), kt = pre_key_tile(c);
+  const int row_blocks = pre_row_blocks(c, a.max_new);
   PreScratch sc{};
   sc.nsplit = pre_splits(c, a.max_new);
   if (sc.nsplit > 1) {
     sc.part = static_cast<float*>(scratch);
     sc.ml = sc.part + static_cast<long long>(c.n_seq) * a.max_new * c.hq * sc.nsplit * c.dh;
   }
-  const long long total = static_cast<long long>(row_blocks) * c.hkv * c.n_seq * sc.nsplit;
-  if (total > (1ll << 31) - 1) return hipErrorInvalidValue;
-#define GMC_PREFILL(T, DH)                                                                                    \
-  case DH:                                                                                                    \
+  // runs of 32 blocks; shorter ones where that leaves an XCD fewer than eight
+  const long long items = static_cast<long long>(row_blocks) * sc.nsplit, heads = static_cast<long long>(c.hkv) * c.n_seq;
+  sc.run = static_cast<int>(std::max<long long>(1, std::min<long long>(32, items * heads / 64)));
+  const long long units = (items + sc.run - 1) / sc.run * heads, total = (units + 7) / 8 * 8 * sc.run;
+#define GMC_PREFILL(T, DH)                                                                                       \
+  case DH:                                                                                                       \
     hipLaunchKernelGGL((prefill_kernel<T, DH>), dim3(static_cast<unsigned>(total)), dim3(64 * kPreWaves), 0, st, c, a, sc, \
-                       row_blocks, static_cast<int>(total));                                                  \
+                       row_blocks); \
     break;
-#define GMC_PREFILL_ALL(T)                                                                                    \
-  switch (c.dh) {                                                                                             \
-    GMC_PREFILL(T, 32) GMC_PREFILL(T, 64) GMC_PREFILL(T, 96) GMC_PREFILL(T, 128)                              \
-    GMC_PREFILL(T, 160) GMC_PREFILL(T, 192) GMC_PREFILL(T, 224) GMC_PREFILL(T, 256)                           \
-    default: return hipErrorInvalidValue;                                                                     \
+#define GMC_PREFILL_ALL(T)                                                                                       \
+  switch (c.dh) {                                                                                                \
+    GMC_PREFILL(T, 32) GMC_PREFILL(T, 64) GMC_PREFILL(T, 96) GMC_PREFILL(T, 128)                                 \
+    GMC_PREFILL(T, 160) GMC_PREFILL(T, 192) GMC_PREFILL(T, 224) GMC_PREFILL(T, 256)                              \
+    default: return hipErrorInvalidValue;                                                                        \
   }
   if (c.dtype == 0) { GMC_PREFILL_ALL(float) } else { GMC_PREFILL_ALL(bf16_t) }
 #undef GMC_PREFILL_ALL
@@ -548,9 +634,9 @@ hipError_t launch_cache_prefill(const CacheView& c, const AttendArgs& a, void* s
   if (sc.nsplit > 1) {
     const dim3 grid((a.max_new + 3) / 4, c.hq, c.n_seq);
     if (c.dtype == 0)
-      hipLaunchKernelGGL(prefill_join_kernel<float>, grid, dim3(256), 0, st, c, a, sc, kt);
+      hipLaunchKernelGGL(prefill_join_kernel<float>, grid, dim3(256), 0, st, c, a, sc);
     else
-      hipLaunchKernelGGL(prefill_join_kernel<bf16_t>, grid, dim3(256), 0, st, c, a, sc, kt);
+      hipLaunchKernelGGL(prefill_join_kernel<bf16_t>, grid, dim3(256), 0, st, c, a, sc);
   }
   return hipGetLastError();
 }
