@@ -689,9 +689,18 @@ class KvCache:
         self.n_seq, self.slots = page_table.shape[0], page_table.shape[1] * page
         self.n_q_heads, self.n_kv_heads, self.head_dim = n_q_heads, hkv, dh
         ptr = (lambda t: None if t is None else t.data_ptr())
+        self._scale = dh ** -0.5
+        self._index_of_device = self.device.index
+        self._current_device = torch.cuda.current_device
+        # (the address alone: a Stream object takes longer than the call)
+        self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+            (lambda i: torch.cuda.current_stream(i).cuda_stream)
+        self._entry = {n: getattr(lib(), n) for n in SIGNATURES if n.startswith("gmc_cache_")}
+        self._need = {}
         self.desc = GmcCache(GMC_BF16 if self.dtype == torch.bfloat16 else GMC_F32, n_q_heads, hkv, dh, page,
                              page_table.shape[1], n_pages, self.n_seq, ptr(k_pages), ptr(v_pages), ptr(page_table),
                              ptr(lens), ptr(seen), ptr(slot_pos), ptr(weights))
+        self._ref = ctypes.byref(self.desc)
 
     @classmethod
     def create(cls, *, n_seq, slots, n_q_heads, n_kv_heads, head_dim, dtype, device="cuda", page_size=64,
@@ -710,37 +719,43 @@ class KvCache:
                         weights=torch.zeros(shape, dtype=torch.float32, device=device))
         return cls(*pages, table, lens, n_q_heads=n_q_heads, **more)
 
-    def _on_device(self):
-        # the current device is the cache's almost always
-        torch = self.torch
-        return None if torch.cuda.current_device() == self.device.index else torch.cuda.device(self.device)
-
-    def _call(self, name, fn, *args):
-        torch = self.torch
-        guard = self._on_device()
-        if guard is None:
-            code = fn(self.desc, *args, torch.cuda.current_stream().cuda_stream)
+    def _call(self, name, *args):
+        """The entry point on the current stream of the cache's device, which is
+        the current device almost always."""
+        if self._current_device() == self._index_of_device:
+            code = self._entry[name](self._ref, *args, self._raw_stream(self._index_of_device))
         else:
-            with guard:
-                code = fn(self.desc, *args, torch.cuda.current_stream().cuda_stream)
-        _check(code, name)
+            with self.torch.cuda.device(self.device):
+                code = self._entry[name](self._ref, *args, self._raw_stream(self._index_of_device))
+        if code != GMC_OK:
+            _check(code, name)
 
-    def _bytes(self, name, need):
-        if need < 0:
-            _check(int(need), name)
-        return self.torch.empty(need, dtype=self.torch.uint8, device=self.device) if need else None
+    def _scratch(self, name, what):
+        """(tensor or None, its address, its bytes) for a call; sizes are asked for
+        once for each `what`, the memory is torch's, of the call's own."""
+        need = self._need.get((name, what))
+        if need is None:
+            need = self._entry[name + "_bytes"](self._ref, what)
+            if need < 0:
+                _check(int(need), name)
+            self._need[name, what] = need
+        if need == 0:
+            return None, None, 0
+        x = self.torch.empty(need, dtype=self.torch.uint8, device=self.device)
+        return x, x.data_ptr(), need
 
     def _rows(self, name, x, heads):
         """Tokens x heads x head_dim in the cache's dtype, each token's heads in
         one run; returns the tokens' stride."""
-        if x.dim() != 3 or x.shape[1] != heads or x.shape[2] != self.head_dim or x.dtype != self.dtype:
+        shape, strides, row = x.shape, x.stride(), heads * self.head_dim
+        if len(shape) != 3 or shape[1] != heads or shape[2] != self.head_dim or x.dtype != self.dtype:
             raise ValueError(f"{name} must be {self.dtype} [tokens][{heads}][{self.head_dim}], got {x.dtype} "
-                             f"{tuple(x.shape)}")
+                             f"{tuple(shape)}")
         if x.device != self.device:
             raise ValueError(f"{name} must be on the cache's device {self.device}; got {x.device}")
-        stride = x.stride(0) if x.shape[0] > 1 else heads * self.head_dim
-        if x.stride(2) != 1 or (heads > 1 and x.stride(1) != self.head_dim) or stride < heads * self.head_dim:
-            raise ValueError(f"{name} must hold each token's heads in one run, got strides {x.stride()}")
+        stride = strides[0] if shape[0] > 1 else row
+        if strides[2] != 1 or (heads > 1 and strides[1] != self.head_dim) or stride < row:
+            raise ValueError(f"{name} must hold each token's heads in one run, got strides {strides}")
         return stride
 
     def _index(self, name, x, shape):
@@ -772,7 +787,7 @@ class KvCache:
             first, taken = None, self._index("src", src, (self.n_seq, max_new))
         else:
             (first, max_new), taken = self._new(rows, starts, max_new), None
-        self._call("gmc_cache_append", gmc_cache_append, k.data_ptr(), v.data_ptr(), sk, sv, rows, first, taken, max_new)
+        self._call("gmc_cache_append", k.data_ptr(), v.data_ptr(), sk, sv, rows, first, taken, max_new)
 
     def _outputs(self, q, out, lse):
         torch = self.torch
@@ -798,11 +813,10 @@ class KvCache:
         stride = self._rows("q", q, self.n_q_heads)
         first, max_new = self._new(q.shape[0], starts, max_new)
         out, ls = self._outputs(q, out, lse)
-        need = gmc_cache_prefill_bytes(self.desc, max_new)
-        ws = self._bytes("gmc_cache_prefill", need)
-        self._call("gmc_cache_prefill", gmc_cache_prefill, q.data_ptr(), stride, q.shape[0], first, max_new,
-                   self.head_dim ** -0.5 if scale is None else scale, window, sinks, out.data_ptr(),
-                   None if ls is None else ls.data_ptr(), None if ws is None else ws.data_ptr(), need)
+        ws, at, size = self._scratch("gmc_cache_prefill", max_new)
+        self._call("gmc_cache_prefill", q.data_ptr(), stride, q.shape[0], first, max_new,
+                   self._scale if scale is None else scale, window, sinks, out.data_ptr(),
+                   None if ls is None else ls.data_ptr(), at, size)
         return out if ls is None else (out, ls)
 
     def decode(self, q, *, window=0, sinks=0, scale=None, accumulate=False, lse=False, out=None):
@@ -813,20 +827,16 @@ class KvCache:
         if q.shape[0] != self.n_seq:
             raise ValueError(f"q must hold one token for each of {self.n_seq} sequences, got {q.shape[0]}")
         out, ls = self._outputs(q, out, lse)
-        need = gmc_cache_decode_bytes(self.desc, accumulate)
-        ws = self._bytes("gmc_cache_decode", need)
-        self._call("gmc_cache_decode", gmc_cache_decode, q.data_ptr(), stride,
-                   self.head_dim ** -0.5 if scale is None else scale, window, sinks, accumulate, out.data_ptr(),
-                   None if ls is None else ls.data_ptr(), None if ws is None else ws.data_ptr(), need)
+        ws, at, size = self._scratch("gmc_cache_decode", 1 if accumulate else 0)
+        self._call("gmc_cache_decode", q.data_ptr(), stride, self._scale if scale is None else scale, window, sinks,
+                   1 if accumulate else 0, out.data_ptr(), None if ls is None else ls.data_ptr(), at, size)
         return out if ls is None else (out, ls)
 
     def evict(self, budget, *, sinks=0, recent=0):
         """gmc_cache_evict: every sequence keeps at most ``budget`` rows a kv
         head, the first ``sinks`` and last ``recent`` positions among them."""
-        need = gmc_cache_evict_bytes(self.desc, budget)
-        ws = self._bytes("gmc_cache_evict", need)
-        self._call("gmc_cache_evict", gmc_cache_evict, budget, sinks, recent, None if ws is None else ws.data_ptr(),
-                   need)
+        ws, at, size = self._scratch("gmc_cache_evict", budget)
+        self._call("gmc_cache_evict", budget, sinks, recent, at, size)
 
 
 def gmc_timing_enable(enable: bool) -> int:

@@ -31,7 +31,7 @@
 namespace gmc {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr int kDecodeWaves = 4;
+constexpr int kDecodeWaves = 4, kDecodeShort = 8;   // waves of a block; where one block does a whole sequence
 
 // Keys a wave takes at a time.
 template <typename T> constexpr int kHalves = sizeof(T) == 2 ? 2 : 1;
@@ -87,20 +87,20 @@ template <int N> __device__ __forceinline__ Raw<N> load_raw(const void* p) {
   return r;
 }
 
-template <typename T, int DH>
-__global__ void __launch_bounds__(64 * kDecodeWaves)
+template <typename T, int DH, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES)
 decode_split_kernel(CacheView c, AttendArgs a, DecodeScratch sc, int qtiles) {
   constexpr int H = kHalves<T>, TK = 16 * H, NS = DH / 32;
   // dims a lane loads of a V row: up to 16 bytes, 16 lanes covering whole runs
   constexpr int VEC = sizeof(T) == 2 ? (DH % 128 == 0 ? 8 : DH % 64 == 0 ? 4 : 2) : (DH % 64 == 0 ? 4 : 2);
   constexpr int NB = DH / (16 * VEC), W = VEC * sizeof(T) / 4;
-  __shared__ float red[kDecodeWaves / 2][16 * DH];
-  __shared__ float stat[kDecodeWaves][2][16];
+  __shared__ float red[WAVES / 2][16 * DH];
+  __shared__ float stat[WAVES][2][16];
   const int split = blockIdx.x, h = blockIdx.y / qtiles, qt = blockIdx.y % qtiles, b = blockIdx.z;
   const int lane = threadIdx.x & 63, w = wave_id(), i16 = lane & 15, g = lane >> 4;
   const int len = cache_len(c, b);
   const TileRange tr = tile_range(len, a.window, a.sinks, c.slot_pos == nullptr, TK);
-  const int ns = used_splits(tr.count, sc.nsplit);
+  const int ns = WAVES == kDecodeWaves ? used_splits(tr.count, sc.nsplit) : 1;
   if (split >= ns) return;
   const int t0 = static_cast<int>(static_cast<long long>(tr.count) * split / ns);
   const int t1 = static_cast<int>(static_cast<long long>(tr.count) * (split + 1) / ns);
@@ -158,7 +158,7 @@ decode_split_kernel(CacheView c, AttendArgs a, DecodeScratch sc, int qtiles) {
 
   int tile = t0 + w;
   if (tile < t1) load(tile);
-  for (; tile < t1; tile += kDecodeWaves) {
+  for (; tile < t1; tile += WAVES) {
     // keys that are not seen: only in the last tile, at the window's edges and
     // on pages that are none
     bool whole = slot0 + TK <= len && (!a.window || (!pos && len - 1 - slot0 < a.window));
@@ -265,7 +265,7 @@ decode_split_kernel(CacheView c, AttendArgs a, DecodeScratch sc, int qtiles) {
           for (int j = 0; j < VEC; ++j)
             o[n][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[0][r][n].u[j]), x[0][r], o[n][j], 0, 0, 0);
     }
-    if (tile + kDecodeWaves < t1) load(tile + kDecodeWaves);
+    if (tile + WAVES < t1) load(tile + WAVES);
   }
 
   // the waves' parts on their common maximum, added in a fixed order
@@ -274,18 +274,18 @@ decode_split_kernel(CacheView c, AttendArgs a, DecodeScratch sc, int qtiles) {
   __syncthreads();
   float mb = stat[0][0][i16];
 #pragma unroll
-  for (int u = 1; u < kDecodeWaves; ++u) mb = fmaxf(mb, stat[u][0][i16]);
+  for (int u = 1; u < WAVES; ++u) mb = fmaxf(mb, stat[u][0][i16]);
   const float base = mb == -INFINITY ? 0.f : mb;
   float lb = 0.f;
 #pragma unroll
-  for (int u = 0; u < kDecodeWaves; ++u) lb += stat[u][1][i16] * __builtin_amdgcn_exp2f(stat[u][0][i16] - base);
+  for (int u = 0; u < WAVES; ++u) lb += stat[u][1][i16] * __builtin_amdgcn_exp2f(stat[u][0][i16] - base);
   const float f = __builtin_amdgcn_exp2f(m - base);
 #pragma unroll
   for (int n = 0; n < NB; ++n)
 #pragma unroll
     for (int j = 0; j < VEC; ++j) o[n][j] *= f;
 #pragma unroll
-  for (int step = kDecodeWaves / 2; step >= 1; step /= 2) {
+  for (int step = WAVES / 2; step >= 1; step /= 2) {
     if (w >= step && w < 2 * step) {
 #pragma unroll
       for (int n = 0; n < NB; ++n)
@@ -331,12 +331,29 @@ decode_split_kernel(CacheView c, AttendArgs a, DecodeScratch sc, int qtiles) {
   if (a.lse && g == 0) a.lse[row] = lb == 0.f ? -INFINITY : (mb + __builtin_amdgcn_logf(lb)) * kLn2;
 }
 
+// The maximum and sum (both base 2) of a row over its splits.
+__device__ __forceinline__ void join_stats(const float* ml, int ns, float* m_out, float* l_out) {
+  const int lane = threadIdx.x & 63;
+  float m = -INFINITY, l = 0.f;
+  for (int s = lane; s < ns; s += 64) {
+    const float2 y = *reinterpret_cast<const float2*>(ml + 2 * s);
+    const float mn = fmaxf(m, y.x), base = mn == -INFINITY ? 0.f : mn;
+    l = l * __builtin_amdgcn_exp2f(m - base) + y.y * __builtin_amdgcn_exp2f(y.x - base);
+    m = mn;
+  }
+  const float mw = wave_max(m), base = mw == -INFINITY ? 0.f : mw;
+  *l_out = wave_sum(l * __builtin_amdgcn_exp2f(m - base));
+  *m_out = mw;
+}
+
 // Joins a sequence's splits.  blockIdx.x < hg: output and lse of one query
-// head of the kv head; above: the weights of one run of 1024 slots.
+// head of the kv head, its splits shared by the block's waves; above: the
+// weights of one run of 1024 slots, for which each wave first takes the lse of
+// some heads.
 template <typename T>
 __global__ void __launch_bounds__(256)
 decode_join_kernel(CacheView c, AttendArgs a, DecodeScratch sc, int tk) {
-  __shared__ float red[4][256];
+  __shared__ __align__(16) float red[4][256];
   __shared__ float lse2[kCacheMaxHeads];
   const int h = blockIdx.y, b = blockIdx.z, lane = threadIdx.x & 63, w = wave_id();
   const int len = cache_len(c, b);
@@ -345,23 +362,35 @@ decode_join_kernel(CacheView c, AttendArgs a, DecodeScratch sc, int tk) {
   if (static_cast<int>(blockIdx.x) < c.hg) {
     const long long row = static_cast<long long>(b) * c.hq + h * c.hg + blockIdx.x;
     const float* ml = sc.ml + row * sc.nsplit * 2;
-    float m = -INFINITY;
-    for (int s = lane; s < ns; s += 64) m = fmaxf(m, ml[2 * s]);
-    m = wave_max(m);
+    const float* part = sc.part + row * sc.nsplit * c.dh + 4 * lane;
+    const bool mine = 4 * lane < c.dh;
+    constexpr int kFlight = 4;
+    floatx4 o = {0.f, 0.f, 0.f, 0.f};
+    float m, l;
+    // (the first parts are on their way while the statistics are taken)
+    floatx4 x[kFlight];
+    auto load = [&](int s0) {
+#pragma unroll
+      for (int e = 0; e < kFlight; ++e) {
+        const int s = min(s0 + 4 * e, ns - 1);
+        x[e] = mine ? *reinterpret_cast<const floatx4*>(part + static_cast<long long>(s) * c.dh) : floatx4{0.f, 0.f, 0.f, 0.f};
+      }
+    };
+    load(w);
+    join_stats(ml, ns, &m, &l);
     const float base = m == -INFINITY ? 0.f : m;
-    float l = 0.f;
-    for (int s = lane; s < ns; s += 64) l += ml[2 * s + 1] * __builtin_amdgcn_exp2f(ml[2 * s] - base);
-    l = wave_sum(l);
-    float o[4] = {0.f, 0.f, 0.f, 0.f};
-    const float* part = sc.part + row * sc.nsplit * c.dh;
-    for (int s = w; s < ns; s += 4) {
-      const float f = __builtin_amdgcn_exp2f(ml[2 * s] - base);
+    for (int s0 = w; s0 < ns; s0 += 4 * kFlight) {
+      if (s0 > w) load(s0);
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (lane + 64 * e < c.dh) o[e] += f * part[static_cast<long long>(s) * c.dh + lane + 64 * e];
+      for (int e = 0; e < kFlight; ++e) {
+        const int s = s0 + 4 * e;
+        if (s >= ns) break;
+        const float f = __builtin_amdgcn_exp2f(ml[2 * s] - base);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) o[u] += f * x[e][u];
+      }
     }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) red[w][lane + 64 * e] = o[e];
+    *reinterpret_cast<floatx4*>(&red[w][4 * lane]) = o;
     __syncthreads();
     const int d = threadIdx.x;
     if (d < c.dh) {
@@ -373,35 +402,40 @@ decode_join_kernel(CacheView c, AttendArgs a, DecodeScratch sc, int tk) {
   }
   const int s0 = (static_cast<int>(blockIdx.x) - c.hg) * 1024;
   if (s0 >= len) return;
+  const int s = s0 + 4 * threadIdx.x;
+  // tiles that no query looks at have no logits
+  const int tile = s / tk;
+  const bool mine = s < len && !(tile >= tr.first && tile < tr.first + tr.skip);
+  const float* logits = sc.logits + (static_cast<long long>(b) * c.hq + h * c.hg) * c.cap + (mine ? s : 0);
+  constexpr int kFlight = 8;
+  floatx4 x[kFlight], add = {0.f, 0.f, 0.f, 0.f};
+  auto load = [&](int head) {
+#pragma unroll
+    for (int e = 0; e < kFlight; ++e)
+      x[e] = *reinterpret_cast<const floatx4*>(logits + static_cast<long long>(min(head + e, c.hg - 1)) * c.cap);
+  };
+  if (mine) load(0);
   for (int head = w; head < c.hg; head += 4) {
-    const float* ml = sc.ml + (static_cast<long long>(b) * c.hq + h * c.hg + head) * sc.nsplit * 2;
-    float m = -INFINITY;
-    for (int s = lane; s < ns; s += 64) m = fmaxf(m, ml[2 * s]);
-    m = wave_max(m);
-    const float base = m == -INFINITY ? 0.f : m;
-    float l = 0.f;
-    for (int s = lane; s < ns; s += 64) l += ml[2 * s + 1] * __builtin_amdgcn_exp2f(ml[2 * s] - base);
-    l = wave_sum(l);
+    float m, l;
+    join_stats(sc.ml + (static_cast<long long>(b) * c.hq + h * c.hg + head) * sc.nsplit * 2, ns, &m, &l);
     // nothing seen: every logit is -inf, and any finite value gives 0
     if (lane == 0) lse2[head] = l == 0.f ? 0.f : m + __builtin_amdgcn_logf(l);
   }
   __syncthreads();
-  const int s = s0 + 4 * threadIdx.x;
-  if (s >= len) return;
-  // tiles that no query looks at have no logits
-  const int tile = s / tk;
-  if (tile >= tr.first && tile < tr.first + tr.skip) return;
-  floatx4 add = {0.f, 0.f, 0.f, 0.f};
-  for (int head = 0; head < c.hg; ++head) {
-    const floatx4 x = *reinterpret_cast<const floatx4*>(
-        sc.logits + (static_cast<long long>(b) * c.hq + h * c.hg + head) * c.cap + s);
+  if (!mine) return;
+  for (int head = 0; head < c.hg; head += kFlight) {
+    if (head > 0) load(head);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) add[e] += __builtin_amdgcn_exp2f(x[e] - lse2[head]);
+    for (int e = 0; e < kFlight; ++e) {
+      if (head + e >= c.hg) break;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) add[u] += __builtin_amdgcn_exp2f(x[e][u] - lse2[head + e]);
+    }
   }
   float* to = c.weights + (static_cast<long long>(b) * c.hkv + h) * c.cap + s;
 #pragma unroll
-  for (int e = 0; e < 4; ++e)
-    if (s + e < len) to[e] += add[e];
+  for (int u = 0; u < 4; ++u)
+    if (s + u < len) to[u] += add[u];
 }
 
 // Splits of a call: enough blocks for the chip, and no more than there are
@@ -415,18 +449,45 @@ static int decode_splits(const CacheView& c, int qtiles) {
 
 static int decode_qtiles(const CacheView& c) { return (c.hg + 15) / 16; }
 
+// Caches of at most two tiles a wave: one block a head and no second kernel.
+static bool decode_short(const CacheView& c, bool accumulate) {
+  return !accumulate && c.dh <= 128 && c.cap <= 2 * kDecodeShort * (c.dtype == 0 ? 16 : 32);
+}
+
 long long decode_scratch_bytes(const CacheView& c, bool accumulate) {
-  const int ns = decode_splits(c, decode_qtiles(c));
+  const int ns = decode_short(c, accumulate) ? 1 : decode_splits(c, decode_qtiles(c));
   if (ns == 1 && !accumulate) return 0;
   const long long rows = static_cast<long long>(c.n_seq) * c.hq;
   return 4 * rows * ns * (c.dh + 2) + (accumulate ? 4 * rows * c.cap : 0);
 }
 
+template <typename T>
+static hipError_t start_decode(const CacheView& c, const AttendArgs& a, const DecodeScratch& sc, int qt, bool one_block,
+                               hipStream_t st) {
+  const dim3 grid(sc.nsplit, c.hkv * qt, c.n_seq);
+#define GMC_DECODE(DH, WAVES)                                                                                        \
+  case DH:                                                                                                           \
+    hipLaunchKernelGGL((decode_split_kernel<T, DH, WAVES>), grid, dim3(64 * WAVES), 0, st, c, a, sc, qt);            \
+    return hipGetLastError();
+#define GMC_DECODE_NARROW(WAVES) GMC_DECODE(32, WAVES) GMC_DECODE(64, WAVES) GMC_DECODE(96, WAVES) GMC_DECODE(128, WAVES)
+  if (one_block) {
+    switch (c.dh) { GMC_DECODE_NARROW(kDecodeShort) default: return hipErrorInvalidValue; }
+  }
+  switch (c.dh) {
+    GMC_DECODE_NARROW(kDecodeWaves)
+    GMC_DECODE(160, kDecodeWaves) GMC_DECODE(192, kDecodeWaves) GMC_DECODE(224, kDecodeWaves) GMC_DECODE(256, kDecodeWaves)
+    default: return hipErrorInvalidValue;
+  }
+#undef GMC_DECODE_NARROW
+#undef GMC_DECODE
+}
+
 hipError_t launch_cache_decode(const CacheView& c, const AttendArgs& a, bool accumulate, void* scratch,
                                hipStream_t st) {
   const int qt = decode_qtiles(c), tk = c.dtype == 0 ? 16 : 32;
+  const bool one_block = decode_short(c, accumulate);
   DecodeScratch sc{};
-  sc.nsplit = decode_splits(c, qt);
+  sc.nsplit = one_block ? 1 : decode_splits(c, qt);
   const bool join = sc.nsplit > 1 || accumulate;
   if (join) {
     const long long rows = static_cast<long long>(c.n_seq) * c.hq;
@@ -434,25 +495,14 @@ hipError_t launch_cache_decode(const CacheView& c, const AttendArgs& a, bool acc
     sc.part = static_cast<float*>(scratch) + (accumulate ? rows * c.cap : 0);
     sc.ml = sc.part + rows * sc.nsplit * c.dh;
   }
-  const dim3 grid(sc.nsplit, c.hkv * qt, c.n_seq);
-#define GMC_DECODE(T, DH)                                                                                  \
-  case DH: hipLaunchKernelGGL((decode_split_kernel<T, DH>), grid, dim3(64 * kDecodeWaves), 0, st, c, a, sc, qt); break;
-#define GMC_DECODE_ALL(T)                                                                                  \
-  switch (c.dh) {                                                                                          \
-    GMC_DECODE(T, 32) GMC_DECODE(T, 64) GMC_DECODE(T, 96) GMC_DECODE(T, 128)                               \
-    GMC_DECODE(T, 160) GMC_DECODE(T, 192) GMC_DECODE(T, 224) GMC_DECODE(T, 256)                            \
-    default: return hipErrorInvalidValue;                                                                  \
-  }
-  if (c.dtype == 0) { GMC_DECODE_ALL(float) } else { GMC_DECODE_ALL(bf16_t) }
-#undef GMC_DECODE_ALL
-#undef GMC_DECODE
-  if (join) {
-    const dim3 jgrid(c.hg + (accumulate ? (c.cap + 1023) / 1024 : 0), c.hkv, c.n_seq);
-    if (c.dtype == 0)
-      hipLaunchKernelGGL(decode_join_kernel<float>, jgrid, dim3(256), 0, st, c, a, sc, tk);
-    else
-      hipLaunchKernelGGL(decode_join_kernel<bf16_t>, jgrid, dim3(256), 0, st, c, a, sc, tk);
-  }
+  const hipError_t err =
+      c.dtype == 0 ? start_decode<float>(c, a, sc, qt, one_block, st) : start_decode<bf16_t>(c, a, sc, qt, one_block, st);
+  if (err != hipSuccess || !join) return err;
+  const dim3 jgrid(c.hg + (accumulate ? (c.cap + 1023) / 1024 : 0), c.hkv, c.n_seq);
+  if (c.dtype == 0)
+    hipLaunchKernelGGL(decode_join_kernel<float>, jgrid, dim3(256), 0, st, c, a, sc, tk);
+  else
+    hipLaunchKernelGGL(decode_join_kernel<bf16_t>, jgrid, dim3(256), 0, st, c, a, sc, tk);
   return hipGetLastError();
 }
 
