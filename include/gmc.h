@@ -598,6 +598,8 @@ int gmc_cache_append(const gmc_cache* cache, const void* k, const void* v, int64
  *   starts  [n_seq + 1] int32: sequence b's rows of q; at most max_new of them
  *           are computed; NULL: max_new each.  Rows of out that belong to no
  *           sequence are left as they are
+ *   max_new the queries of a sequence's kv head, in blocks of 128, times n_seq
+ *           and n_kv_heads must not be more than 2^23 blocks
  *   out     [rows][n_q_heads][head_dim] dtype, 16-byte aligned
  *   lse     [rows][n_q_heads] float32 or NULL
  */
@@ -628,7 +630,9 @@ int gmc_cache_decode(const gmc_cache* cache, const void* q, int64_t q_stride, fl
  * below the budget whose rows leave are filled: the i-th of them takes the
  * i-th kept slot at or above the budget - K, V, position and weight.  lens
  * becomes `budget`.  Needs weights, slot_pos and seen; sinks + recent <=
- * budget.
+ * budget.  The slots of such a sequence should be held: a kept row moves only
+ * from a page that is one to a page that is one, while its weight and position
+ * move all the same.
  */
 int64_t gmc_cache_evict_bytes(const gmc_cache* cache, int64_t budget);
 int gmc_cache_evict(const gmc_cache* cache, int64_t budget, int64_t sinks, int64_t recent, void* workspace,

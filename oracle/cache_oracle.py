@@ -60,7 +60,7 @@ def attend(cache, q, first, counts, scale, window=0, sinks=0):
     counts[b].  Returns a dict of arrays over the rows (rows of no sequence NaN):
     out, lse; probs[b][h][s], the weights a sequence's queries put on each slot;
     and what error bounds need: mass = sum_s a_s |v_s|, size = the largest
-    scale * sum_d |q_d k_d| and most = keys seen."""
+    |scale| sum_d |q_d k_d| and most = keys seen."""
     rows, hq, dh = q.shape
     hkv = cache["k"].shape[1]
     hg = hq // hkv
@@ -89,7 +89,7 @@ def attend(cache, q, first, counts, scale, window=0, sinks=0):
                     a = e / e.sum()
                     out[r, j], lse[r, j] = a @ v[idx], m + np.log(e.sum())
                     mass[r, j] = a @ np.abs(v[idx])
-                    size[r, j] = scale * (np.abs(k[idx]) @ np.abs(q[r, j])).max()
+                    size[r, j] = abs(scale) * (np.abs(k[idx]) @ np.abs(q[r, j])).max()
                     most[r, j] = len(idx)
                     probs[b, h, idx] += a
     return dict(out=out, lse=lse, mass=mass, size=size, most=most, probs=probs)

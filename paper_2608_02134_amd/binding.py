@@ -676,6 +676,7 @@ class KvCache:
     ``page_table`` [n_seq][max_pages] int32, ``lens`` [n_seq] int32; for a cache
     that evicts also ``seen`` [n_seq] int32, ``slot_pos``
     [n_seq][n_kv_heads][slots] int32 and ``weights`` of the same shape, float32.
+    The calls work on these very tensors: change them in place.
     """
 
     def __init__(self, k_pages, v_pages, page_table, lens, *, n_q_heads, slot_pos=None, seen=None, weights=None):

@@ -42,6 +42,9 @@ struct AttendArgs {
 };
 
 #ifdef __HIPCC__
+// Four integers of an array that is aligned as one is.
+typedef int32_t i32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+
 __device__ __forceinline__ int cache_len(const CacheView& c, int b) { return min(max(c.lens[b], 0), c.cap); }
 
 // Row of slot s in the pages of head h, in rows of dh elements; -1: not held.

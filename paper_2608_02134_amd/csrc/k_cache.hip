@@ -139,7 +139,6 @@ __device__ __forceinline__ uint32_t evict_key(float w, bool safe) {
 // strings them together.
 constexpr int kEvictBins = 2048, kEvictList = 1024, kEvictRuns = 16, kEvictHead = 64;
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
-typedef int32_t i32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 
 // Scratch memory: the lengths of the runs' lists, then the lists.
 struct EvictLists {

@@ -355,7 +355,7 @@ prefill_kernel(CacheView c, AttendArgs a, PreScratch sc, int row_blocks) {
           const bool on = (ok >> (2 * kb + (j >> 1))) & 1u;
           int p[4] = {s, s + 1, s + 2, s + 3};
           if (pos) {
-            const int4 y = on ? *reinterpret_cast<const int4*>(pos + s) : make_int4(0, 0, 0, 0);
+            const i32x4_any y = on ? *reinterpret_cast<const i32x4_any*>(pos + s) : i32x4_any{0, 0, 0, 0};
             p[0] = y.x; p[1] = y.y; p[2] = y.z; p[3] = y.w;
           }
 #pragma unroll
@@ -372,9 +372,10 @@ prefill_kernel(CacheView c, AttendArgs a, PreScratch sc, int row_blocks) {
       for (int i = 0; i < 16; ++i) mt = fmaxf(mt, x[kb][i]);
     mt = fmaxf(mt, xor_lane<32>(mt));
     // the running maximum follows in steps of at least 8 (base 2): weights stay
-    // below 2^8 and most tiles rescale nothing
+    // below 2^8 and most tiles rescale nothing.  Each query's own: its bits do
+    // not depend on its neighbours'
     if (__any(mt > m + slack)) {
-      const float mn = fmaxf(m, mt);
+      const float mn = mt > m + slack ? mt : m;
       const float f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - mn) * cs);
       m = mn;
       l *= f;

@@ -173,3 +173,13 @@ def test_struct_layout_matches_the_c_compiler(tmp_path):
     out = subprocess.run([str(exe)], capture_output=True, text=True, check=True).stdout.split()
     assert [int(x) for x in out] == [getattr(B.GmcCache, n).offset for n in names] + [ctypes.sizeof(B.GmcCache),
                                                                                      B.GMC_CACHE_MAX_HEADS]
+
+
+def test_prefill_of_more_blocks_than_a_grid_holds():
+    """2^23 blocks of 128 (token, head) queries: more are refused before anything
+    is launched, also where one sequence's count alone passes 32 bits."""
+    big = dict(max_pages=1 << 20, n_pages=1 << 20)
+    call = lambda c, n: B.gmc_cache_prefill(c, P, c.n_q_heads * c.head_dim, 1, P, n, 0.1, 0, 0, P, None, P, 1 << 62)  # noqa: E731
+    _refused(call(_cache(n_seq=1, n_q_heads=256, n_kv_heads=1, head_dim=32, **big), 1 << 24), "2^23 blocks")
+    _refused(call(_cache(n_seq=65535, n_q_heads=256, n_kv_heads=256, head_dim=32, **big), 1), "2^23 blocks")
+    _refused(call(_cache(n_seq=3000, n_q_heads=8, n_kv_heads=2, head_dim=64, **big), 100000), "2^23 blocks")

@@ -434,3 +434,256 @@ def test_repeats_bit_for_bit_on_another_stream():
         out2, lse2 = dev.decode(q, accumulate=True, lse=True)
     side.synchronize()
     assert torch.equal(out, out2) and torch.equal(lse, lse2) and torch.equal(w1, dev.weights)
+
+
+# --- calls that a program may make and the cases above do not ---------------------------
+def _unaligned(t):
+    """The same values at an address that is a multiple of 4 bytes only."""
+    x = torch.empty(t.numel() + 5, dtype=t.dtype, device=t.device)
+    for skip in (1, 2, 3, 5):
+        y = x[skip: skip + t.numel()]
+        if y.data_ptr() % 8:
+            break
+    y.copy_(t.reshape(-1))
+    return y.view(t.shape)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_positions_and_weights_at_any_address(dtype):
+    """Prefill, decode, append and eviction with slot_pos and weights that are not
+    16-byte aligned give what they give with aligned ones, bit for bit."""
+    _say(f"unaligned {dtype}")
+    rng = np.random.default_rng(30)
+    c = C.make(rng, dtype=dtype, hq=6, hkv=3, dh=64, page=16, lens=[150, 33], slots=176, positions=True, weights=True)
+    a, b = C.on_gpu(c), C.on_gpu(c)
+    b = C.B.KvCache(b.k_pages, b.v_pages, b.page_table, b.lens, n_q_heads=6, seen=b.seen,
+                    slot_pos=_unaligned(b.slot_pos), weights=_unaligned(b.weights))
+    q = C.to_gpu(C.queries(rng, c, 40), dtype)
+    kv = C.to_gpu(C.rounded(rng.standard_normal((2, 2, 3, 64)), dtype), dtype)
+    got = []
+    for x in (a, b):
+        x.append(kv[:, 0], kv[:, 1])
+        p = x.prefill(q, window=37, sinks=3, lse=True)
+        d = x.decode(q[:2], window=37, sinks=3, accumulate=True, lse=True)
+        x.evict(100, sinks=3, recent=20)
+        got.append([*p, *d, x.slot_pos[0, :, :100], x.weights[0, :, :100], x.lens, x.seen])
+    assert got[1][4].data_ptr() % 16 != 0
+    for x, y in zip(*got):
+        assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("page", [128, 256, 512, 1024])
+def test_large_pages(dtype, page):
+    _say(f"page {page} {dtype}")
+    rng = np.random.default_rng(page)
+    c = C.make(rng, dtype=dtype, hq=6, hkv=2, dh=64, page=page, lens=[1100, 2, page], slots=1100, weights=True)
+    _decode(rng, c, 0, 0, accumulate=True)
+    _prefill(rng, c, [130, 2, 5], 200, 3)
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.11, 0.5])
+def test_scales(scale):
+    """A scale of zero weighs every visible key alike; a negative one is a sign."""
+    _say(f"scale {scale}")
+    for dtype in ("bf16", "f32"):
+        rng = np.random.default_rng(31)
+        c = C.make(rng, dtype=dtype, hq=4, hkv=2, dh=64, page=16, lens=[70, 20], slots=80)
+        q = C.queries(rng, c, 10)
+        dev, x = C.on_gpu(c), C.to_gpu(q, dtype)
+        out, lse = dev.prefill(x, scale=scale, lse=True)
+        C.check_attention(O.attend(c, q, [0, 5], [5, 5], scale), C.host(out), C.host(lse), dtype, 64)
+        out, lse = dev.decode(x[:2], scale=scale, lse=True)
+        C.check_attention(O.attend(c, q[:2], [0, 1], [1, 1], scale), C.host(out), C.host(lse), dtype, 64)
+
+
+def test_most_heads():
+    """256 query heads on one kv head and on 256."""
+    for hq, hkv in ((256, 1), (256, 256)):
+        _say(f"heads {hq} on {hkv}")
+        rng = np.random.default_rng(hkv)
+        c = C.make(rng, dtype="bf16", hq=hq, hkv=hkv, dh=32, page=16, lens=[40, 17], slots=48, weights=True)
+        _decode(rng, c, 0, 0, accumulate=True)
+        _prefill(rng, c, [3, 17], 9, 1)
+
+
+@pytest.mark.parametrize("dtype,cap", [("bf16", 512), ("bf16", 528), ("f32", 256), ("f32", 272)])
+@pytest.mark.parametrize("window", [(0, 0), (100, 3)], ids=str)
+def test_decode_where_one_block_takes_a_sequence_and_just_past(dtype, cap, window):
+    _say(f"decode {dtype} slots {cap} {window}")
+    rng = np.random.default_rng(cap)
+    c = C.make(rng, dtype=dtype, hq=6, hkv=2, dh=96, page=16, lens=[cap, cap - 1, cap - 16, 240, 1], slots=cap)
+    _decode(rng, c, *window)
+
+
+def test_prefill_of_many_blocks():
+    """More blocks than are split over keys, in runs over heads and unlike sequences."""
+    _say("prefill many blocks")
+    rng = np.random.default_rng(32)
+    lens = [700, 3, 650, 1, 333]
+    c = C.make(rng, dtype="bf16", hq=28, hkv=4, dh=64, page=16, lens=lens, slots=704)
+    _prefill(rng, c, lens, 0, 0)
+    _prefill(rng, c, [600, 3, 649, 1, 0], 130, 4)
+
+
+def test_append_of_few_and_many_tokens():
+    for n in (15, 16, 17, 18):
+        _say(f"append {n}")
+        rng = np.random.default_rng(n)
+        c = C.make(rng, dtype="bf16", hq=6, hkv=2, dh=32, page=16, lens=[10, 0, 60], slots=64, positions=True, weights=True)
+        kv = C.rounded(rng.standard_normal((3 * n, 2, 2, 32)), "bf16")
+        dev, x = C.on_gpu(c), C.to_gpu(kv, "bf16")
+        dev.append(x[:, 0], x[:, 1])
+        O.append(c, kv[:, 0], kv[:, 1], [n] * 3, [np.arange(i * n, (i + 1) * n) for i in range(3)])
+        _compare_caches(c, dev)
+
+
+def test_rows_past_max_new_are_not_taken():
+    _say("rows past max_new")
+    rng = np.random.default_rng(33)
+    c = C.make(rng, dtype="bf16", hq=4, hkv=2, dh=64, page=16, lens=[30, 40], slots=64)
+    q = C.queries(rng, c, 20)
+    starts = torch.tensor([2, 12, 20], dtype=torch.int32).cuda()      # 10 and 8 rows, of which 5 each
+    dev, x = C.on_gpu(c), C.to_gpu(q, "bf16")
+    out, lse = torch.full_like(x, 7.0), torch.full((20, 4), 7.0, device="cuda")
+    dev.prefill(x, starts=starts, max_new=5, out=out, lse=lse)
+    took = np.r_[2:7, 12:17]
+    left = np.setdiff1d(np.arange(20), took)
+    C.check_attention(O.attend(c, q, [2, 12], [5, 5], 0.125), C.host(out), C.host(lse), "bf16", 64,
+                      rows=np.isin(np.arange(20), took))
+    assert (out[left] == 7).all() and (lse[left] == 7).all()
+
+
+def test_offsets_past_32_bits():
+    """Pages beyond 2^31 elements: every call gives what it gives on low pages."""
+    _say("far pages")
+    hkv, page, dh, b, per = 8, 64, 128, 2, 5
+    far = (1 << 31) // (hkv * page * dh) + 7             # the first of the far pages
+    shape = (hkv, page, dh)
+    big = [torch.empty((far + b * per, *shape), dtype=torch.bfloat16, device="cuda") for _ in "kv"]
+    low = [torch.randn((b * per, *shape), device="cuda").bfloat16() for _ in "kv"]
+    for x, y in zip(big, low):
+        x[far:] = y
+    got = []
+    g = torch.Generator("cuda").manual_seed(5)
+    q = 2 * torch.randn((20, 32, dh), generator=g, device="cuda").bfloat16()
+    kv = torch.randn((20, 2, hkv, dh), generator=g, device="cuda").bfloat16()
+    w = torch.rand((b, hkv, per * page), generator=g, device="cuda")
+    for pages, base in ((low, 0), (big, far)):
+        table = (base + torch.arange(b * per, device="cuda", dtype=torch.int32)).view(b, per)
+        pos = torch.arange(per * page, device="cuda", dtype=torch.int32).expand(b, hkv, -1).contiguous()
+        lens = torch.tensor([300, 130], dtype=torch.int32, device="cuda")
+        dev = C.B.KvCache(*pages, table, lens, n_q_heads=32, seen=lens.clone(), slot_pos=pos, weights=w.clone())
+        dev.append(kv[:, 0], kv[:, 1])
+        p = dev.prefill(q, lse=True)
+        d = dev.decode(q[:2], accumulate=True, lse=True)
+        dev.evict(150, sinks=2, recent=5)
+        e = dev.decode(q[:2], lse=True)
+        got.append([*p, *d, *e, dev.weights[..., :140], dev.slot_pos[..., :140], dev.lens,
+                    pages[0][base:base + b * per], pages[1][base:base + b * per]])
+    for x, y in zip(*got):
+        assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_captured_prefill_replays(dtype):
+    """A prefill split over keys and joined, and one that is not, in one graph with
+    the appending of their rows."""
+    _say(f"graph prefill {dtype}")
+    rng = np.random.default_rng(34)
+    c = C.make(rng, dtype=dtype, hq=14, hkv=2, dh=64, page=16, lens=[700, 90], slots=720)
+    dev = C.on_gpu(c)
+    kv = torch.zeros((6, 2, 2, 64), dtype=C.DT[dtype], device="cuda")
+    q = torch.zeros((6, 14, 64), dtype=C.DT[dtype], device="cuda")
+    keep = dev.lens.clone()
+
+    def step():
+        dev.lens.copy_(keep)
+        dev.append(kv[:, 0], kv[:, 1])
+        return [*dev.prefill(q, lse=True), *dev.prefill(q[:2], window=9, sinks=1, lse=True)]
+
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for i in range(4):
+        kv.copy_(torch.from_numpy(rng.standard_normal(kv.shape)).cuda())
+        q.copy_(torch.from_numpy(rng.standard_normal(q.shape)).cuda())
+        graph.replay()
+        torch.cuda.synchronize()
+        held = [t.clone() for t in got]
+        for x, y in zip(held, step()):
+            assert torch.equal(x, y), i
+
+
+def test_two_calls_at_once():
+    """Attention calls on one cache on two streams, each with scratch memory of its own."""
+    _say("two streams")
+    rng = np.random.default_rng(35)
+    c = C.make(rng, dtype="bf16", hq=28, hkv=4, dh=128, page=64, lens=[3000, 2500], slots=3008)
+    dev = C.on_gpu(c)
+    q = [C.to_gpu(C.queries(rng, c, 12), "bf16") for _ in range(2)]
+    want = [[*dev.prefill(x, lse=True), *dev.decode(x[:2], lse=True)] for x in q]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in q]
+    for _ in range(5):
+        got = []
+        for x, s in zip(q, streams):
+            with torch.cuda.stream(s):
+                got.append([*dev.prefill(x, lse=True), *dev.decode(x[:2], lse=True)])
+        torch.cuda.synchronize()
+        for x, y in zip(want, got):
+            assert all(torch.equal(u, v) for u, v in zip(x, y))
+
+
+def test_a_query_does_not_depend_on_its_neighbours():
+    """Bit for bit: large logits of other queries of a block change nothing."""
+    _say("neighbours")
+    rng = np.random.default_rng(36)
+    for dtype in ("bf16", "f32"):
+        c = C.make(rng, dtype=dtype, hq=4, hkv=1, dh=64, page=16, lens=[400], slots=400)
+        dev, q = C.on_gpu(c), C.queries(rng, c, 60)
+        out, lse = dev.prefill(C.to_gpu(q, dtype), lse=True)
+        loud = q.copy()
+        loud[1::2] *= 40 * np.linspace(0, 1, 30)[:, None, None]
+        loud = C.rounded(loud, dtype)
+        out2, lse2 = dev.prefill(C.to_gpu(loud, dtype), lse=True)
+        assert torch.equal(out[::2], out2[::2]) and torch.equal(lse[::2], lse2[::2])
+        assert not torch.equal(lse[1::2], lse2[1::2])
+
+
+def test_wrapper_refusals_on_the_device():
+    _say("refusals")
+    rng = np.random.default_rng(37)
+    c = C.make(rng, dtype="bf16", hq=4, hkv=2, dh=64, page=16, lens=[30, 40], slots=64)
+    dev = C.on_gpu(c)
+    q = torch.zeros((2, 4, 64), dtype=torch.bfloat16, device="cuda")
+    k = q[:, :2].contiguous()
+    starts = torch.tensor([0, 1, 2], dtype=torch.int32, device="cuda")
+    for call, what in (
+            (lambda: dev.decode(q.float()), "torch.bfloat16"),
+            (lambda: dev.decode(q[:1]), "one token for each"),
+            (lambda: dev.decode(q.cpu()), "device"),
+            (lambda: dev.decode(q.transpose(0, 1).contiguous().transpose(0, 1)), "in one run"),
+            (lambda: dev.decode(q[:1].expand(2, 4, 64)), "in one run"),
+            (lambda: dev.decode(q, out=torch.empty_like(q, dtype=torch.float32)), "out must"),
+            (lambda: dev.decode(q, lse=torch.empty((2, 4), device="cuda").bfloat16()), "lse must"),
+            (lambda: dev.prefill(q, starts=starts), "max_new"),
+            (lambda: dev.prefill(q, starts=starts.long(), max_new=1), "starts"),
+            (lambda: dev.prefill(q[:, :2]), "tokens"),
+            (lambda: dev.append(k, k[:1]), "tokens"),
+            (lambda: dev.append(k, k, src=starts[None]), "src"),
+            (lambda: dev.append(k, k, starts=starts, max_new=1, src=starts[:2, None].contiguous()), "both"),
+            (lambda: dev.append(torch.cat([k, k[:1]]), torch.cat([k, k[:1]])), "same number")):
+        with pytest.raises(ValueError, match=what):
+            call()
+    for call, what in ((lambda: dev.decode(q, accumulate=True), "weights"),
+                       (lambda: dev.evict(20), "needs"),
+                       (lambda: dev.decode(q, window=-1), "window"),
+                       (lambda: dev.prefill(q, starts=starts, max_new=65), "max_new")):
+        with pytest.raises(RuntimeError, match=what):
+            call()
+    assert dev.lens.tolist() == [30, 40]
