@@ -22,7 +22,6 @@
 #include <limits.h>
 
 #include <algorithm>
-#include <type_traits>
 
 #include "gmc_cache.h"
 #include "gmc_device.h"
@@ -118,7 +117,7 @@ prefill_kernel(CacheView c, AttendArgs a, PreScratch sc, int row_blocks) {
   constexpr int GROUPS = KT / 16;                          // runs of 16 slots, each on one page
   constexpr int LOADS = CPR / 4;                           // 1 KB loads of one run
   __shared__ __align__(16) unsigned char k_even[KT * PITCH], v_even[KT * PITCH], k_odd[KT * PITCH], v_odd[KT * PITCH];
-  __shared__ int special_seen;   // an infinity or NaN was taken out of a tile
+  __shared__ __align__(16) int pos_even[64], pos_odd[64];   // positions of the tiles' slots, if the window asks for them
 
   // Each of the eight XCDs (blocks go to them in turn) works on runs of
   // neighbouring row blocks of a head, whose keys its L2 then holds, and the
@@ -158,19 +157,29 @@ prefill_kernel(CacheView c, AttendArgs a, PreScratch sc, int row_blocks) {
   const int32_t* pos = a.window ? c.slot_pos : nullptr;    // positions matter to the window only
   if (pos) pos += at;
   const int mine = pos && t >= 0 ? pos[t] : t;
-  // exp2(scale log2(e) s): a negative scale goes to the query's sign, and a
+  // exp2(scale log2(e) s): a negative scale goes to the queries' sign, and a
   // scale of zero to one that does not turn a hidden key's -inf into NaN
   const float cs = fmaxf(fabsf(a.scale) * 1.4426950408889634f, 1e-30f);
+
+  const int32_t* table = c.table + static_cast<long long>(b) * c.max_pages;
+  auto slot0 = [&](int it) GMC_INLINE { return (it < wk.sink_tiles ? it : it + wk.skip) * KT; };
+  // The page ids of a tile's runs, one a lane (the first GROUPS lanes): fetched a
+  // tile before its loads start, which would wait for them (3900 of 7100 cycles
+  // a tile), and first looked at there: a look here would wait for all loads on
+  // their way.
+  auto fetch = [&](int it) GMC_INLINE { return table[min(slot0(it) + 16 * (lane & (GROUPS - 1)), c.cap - 1) >> c.shift]; };
+  // Which runs of a tile are on a page.
+  auto on_pages = [&](int it, int ids) GMC_INLINE {
+    const bool on = slot0(it) + 16 * (lane & (GROUPS - 1)) < wk.len && ids >= 0 && ids < c.n_pages;
+    return static_cast<unsigned>(__ballot(on)) & ((1u << GROUPS) - 1u);
+  };
+  int ids0 = fetch(it0), ids1 = fetch(it0 + 1);
 
   uint4 q[NS];
   {
     const T* qp = static_cast<const T*>(a.q) + (wk.first + tok) * a.q_stride + static_cast<long long>(hq) * DH;
-    const uint32_t flip = a.scale < 0.f ? (sizeof(T) == 2 ? 0x80008000u : 0x80000000u) : 0u;
 #pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      q[s] = ld16(reinterpret_cast<const char*>(qp) + 16 * (2 * s + half));
-      q[s].x ^= flip; q[s].y ^= flip; q[s].z ^= flip; q[s].w ^= flip;
-    }
+    for (int s = 0; s < NS; ++s) q[s] = ld16(reinterpret_cast<const char*>(qp) + 16 * (2 * s + half));
   }
   floatx16 o[NB];
 #pragma unroll
@@ -212,26 +221,16 @@ prefill_kernel(CacheView c, AttendArgs a, PreScratch sc, int row_blocks) {
     return kXor ? v_base[0][e] ^ ((sizeof(T) == 2 ? 64 : 128) * n) : v_base[kXor ? 0 : n][e];
   };
 
-  const int32_t* table = c.table + static_cast<long long>(b) * c.max_pages;
   const long long page_bytes = static_cast<long long>(c.page) * PITCH;
-  auto slot0 = [&](int it) GMC_INLINE { return (it < wk.sink_tiles ? it : it + wk.skip) * KT; };
-  // The page ids of a tile's runs, one a lane (the first GROUPS lanes): fetched a
-  // tile before its loads start, which would wait for them (3900 of 7100 cycles
-  // a tile).
-  auto fetch = [&](int it) GMC_INLINE {
-    const int s = slot0(it) + 16 * (lane & (GROUPS - 1));
-    const int id = table[min(s, c.cap - 1) >> c.shift];
-    return it < it1 && s < wk.len ? id : -1;
-  };
   // Starts the loads of a tile; returns which of its runs are on a page.  A wave
   // loads K and V of one run (64 keys a tile), or one of the two (32 keys).
-  auto issue = [&](int it, int ids, shared_u8* ks, shared_u8* vs) GMC_INLINE -> unsigned {
+  auto issue = [&](int it, int ids, shared_u8* ks, shared_u8* vs, shared_u8* ps) GMC_INLINE -> unsigned {
     const int s0 = slot0(it);
+    if (pos && w == 0) __builtin_amdgcn_global_load_lds((const global_u32*)(pos + min(s0 + lane, c.cap - 1)), ps, 4, 0, 0);
     constexpr bool kBoth = GROUPS == kPreWaves;
     static_assert(kBoth || 2 * GROUPS == kPreWaves, "a wave loads K and V of a run, or one of them");
     const int mine = kBoth ? w : w >> 1;
-    const bool on = ids >= 0 && ids < c.n_pages;
-    const unsigned ok = static_cast<unsigned>(__ballot(on)) & ((1u << GROUPS) - 1u);
+    const unsigned ok = on_pages(it, ids);
     const int pid = (ok >> mine) & 1u ? __builtin_amdgcn_readlane(ids, mine) : -1;
     const int s = s0 + 16 * mine, held = pid < 0 ? 0 : wk.len - s;   // rows of the run that are held
     const long long base =
@@ -278,28 +277,25 @@ prefill_kernel(CacheView c, AttendArgs a, PreScratch sc, int row_blocks) {
   auto edge_of_block = [&](int s0, unsigned ok) GMC_INLINE {
     return ok != (1u << GROUPS) - 1u || s0 + KT - 1 > wk.t_min || pos || (a.window && wk.t_max - s0 >= a.window);
   };
-  // One tile; `inner`: every query of the block sees every key of it.  In another,
-  // an infinity or NaN among the values must not reach a query that does not see
-  // it, through a weight of zero: it is taken out here and added at the end.
-  auto compute = [&](auto inner, int it, unsigned ok, shared_u8* ks, shared_u8* vs) GMC_INLINE {
-    constexpr bool kInner = decltype(inner)::value;
+  // An infinity or NaN among the values must not reach a query that does not see
+  // it, through a weight of zero.  That it did shows in the sums, so the block's
+  // tiles are first taken as if there were none; if a sum is not finite, all over
+  // again with care: the infinities and NaN of tiles where some query does not
+  // see some key are taken out, and added at the end.
+  bool care = false;
+  auto compute = [&](int it, unsigned ok, shared_u8* ks, shared_u8* vs, shared_u8* ps) GMC_INLINE {
     const int s0 = slot0(it);
-    bool edge = false;
-    if constexpr (!kInner) {
-#pragma unroll
+    if (care && edge_of_block(s0, ok)) {
+#pragma unroll 1
       for (int x = 0; x < KT * CPR / (64 * kPreWaves); ++x) {
         shared_u8* at = vs + 16 * (64 * kPreWaves * x + static_cast<int>(threadIdx.x));
         u32x4 y = ld_shared<u32x4>(at);
-        if (clean(y)) {
-          *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(at) = y;
-          special_seen = 1;
-        }
+        if (clean(y)) *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(at) = y;
       }
       __syncthreads();
-      if (s0 > wt_max) return;
-      edge = ok != (1u << GROUPS) - 1u || s0 + KT - 1 > wt_min || pos || (a.window && wt_max - s0 >= a.window);
     }
-
+    if (s0 > wt_max) return;
+    const bool all = ok == (1u << GROUPS) - 1u;
     if constexpr (kXor) {
       asm volatile("" : "+v"(k_base[0]));   // (formed in each tile anew)
 #pragma unroll
@@ -345,7 +341,7 @@ prefill_kernel(CacheView c, AttendArgs a, PreScratch sc, int row_blocks) {
     }
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) settle(x[kb]);
-    if (edge) {
+    if (!all || pos || (a.window && s0 < a.sinks)) {
       const int win = a.window ? a.window : INT_MAX;
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
@@ -355,8 +351,9 @@ prefill_kernel(CacheView c, AttendArgs a, PreScratch sc, int row_blocks) {
           const bool on = (ok >> (2 * kb + (j >> 1))) & 1u;
           int p[4] = {s, s + 1, s + 2, s + 3};
           if (pos) {
-            const i32x4_any y = on ? *reinterpret_cast<const i32x4_any*>(pos + s) : i32x4_any{0, 0, 0, 0};
-            p[0] = y.x; p[1] = y.y; p[2] = y.z; p[3] = y.w;
+            const u32x4 y = ld_shared<u32x4>(ps + 4 * sl);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) p[r] = static_cast<int>(y[r]);
           }
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
@@ -364,6 +361,17 @@ prefill_kernel(CacheView c, AttendArgs a, PreScratch sc, int row_blocks) {
             x[kb][4 * j + r] = see ? x[kb][4 * j + r] : -INFINITY;
           }
         }
+    } else if (s0 + KT - 1 > wt_min || (a.window && wt_max - s0 >= a.window)) {
+      // the slots that a query sees are one run: of `span` + 1 from `lo` on (none:
+      // t < 0, then lo is past the tile)
+      const int lo = t < 0 ? INT_MAX : a.window && t >= a.window ? t - a.window + 1 : 0;
+      const unsigned span = t < 0 ? 0u : static_cast<unsigned>(t - lo);
+      const unsigned at = static_cast<unsigned>(s0 + 4 * half) - static_cast<unsigned>(lo);
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          x[kb][i] = at + (32 * kb + 8 * (i >> 2) + (i & 3)) <= span ? x[kb][i] : -INFINITY;
     }
     float mt = x[0][0];
 #pragma unroll
@@ -437,12 +445,6 @@ prefill_kernel(CacheView c, AttendArgs a, PreScratch sc, int row_blocks) {
                                                       o[n], 0, 0, 0);
     }
   };
-  auto step = [&](int it, unsigned ok, shared_u8* ks, shared_u8* vs) GMC_INLINE {
-    if (edge_of_block(slot0(it), ok))
-      compute(std::false_type{}, it, ok, ks, vs);
-    else
-      compute(std::true_type{}, it, ok, ks, vs);
-  };
   // a tile is in shared memory for all waves once each has waited for its loads
   auto arrive = [&]() GMC_INLINE {
     __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
@@ -453,31 +455,50 @@ prefill_kernel(CacheView c, AttendArgs a, PreScratch sc, int row_blocks) {
   shared_u8* const vb0 = (shared_u8*)v_even;
   shared_u8* const kb1 = (shared_u8*)k_odd;
   shared_u8* const vb1 = (shared_u8*)v_odd;
-  if (threadIdx.x == 0) special_seen = 0;   // (seen after the first arrival)
+  shared_u8* const pb0 = (shared_u8*)pos_even;
+  shared_u8* const pb1 = (shared_u8*)pos_odd;
   unsigned ok0 = 0, ok1 = 0;
-  int ids = fetch(it0);
-  if (it0 < it1) ok0 = issue(it0, ids, kb0, vb0);
-  ids = fetch(it0 + 1);
-  for (int it = it0; it < it1; it += 2) {
-    arrive();
-    if (it + 1 < it1) ok1 = issue(it + 1, ids, kb1, vb1);
-    ids = fetch(it + 2);
-    step(it, ok0, kb0, vb0);
-    if (it + 1 >= it1) break;
-    arrive();
-    if (it + 2 < it1) ok0 = issue(it + 2, ids, kb0, vb0);
-    ids = fetch(it + 3);
-    step(it + 1, ok1, kb1, vb1);
+  for (;;) {
+    if (it0 < it1) ok0 = issue(it0, ids0, kb0, vb0, pb0);
+    if (!care && a.scale < 0.f) {
+      constexpr uint32_t kFlip = sizeof(T) == 2 ? 0x80008000u : 0x80000000u;
+#pragma unroll
+      for (int s = 0; s < NS; ++s) { q[s].x ^= kFlip; q[s].y ^= kFlip; q[s].z ^= kFlip; q[s].w ^= kFlip; }
+    }
+    int ids = ids1;
+    for (int it = it0; it < it1; it += 2) {
+      arrive();
+      if (it + 1 < it1) ok1 = issue(it + 1, ids, kb1, vb1, pb1);
+      ids = fetch(it + 2);
+      compute(it, ok0, kb0, vb0, pb0);
+      if (it + 1 >= it1) break;
+      arrive();
+      if (it + 2 < it1) ok0 = issue(it + 2, ids, kb0, vb0, pb0);
+      ids = fetch(it + 3);
+      compute(it + 1, ok1, kb1, vb1, pb1);
+    }
+    asm volatile("s_nop 15\n\ts_nop 7" ::: "memory");   // (see settle)
+    __builtin_amdgcn_sched_barrier(0);
+    if (care) break;
+    float odd = 0.f;   // not zero where a sum is not finite
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) odd = fmaf(o[n][i], 0.f, odd);
+    if (!__syncthreads_or(odd != 0.f)) break;
+    care = true;
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[n][i] = 0.f;
+    m = -INFINITY;
+    l = 0.f;
   }
-  asm volatile("s_nop 15\n\ts_nop 7" ::: "memory");   // (see settle)
-  __builtin_amdgcn_sched_barrier(0);
-  __syncthreads();
-  if (special_seen) {
+  if (care) {
     // the infinities and NaN that were taken out, to the queries that see them
 #pragma unroll 1
     for (int it = it0; it < it1; ++it) {
-      const unsigned ok = static_cast<unsigned>(__ballot(fetch(it) >= 0 && fetch(it) < c.n_pages)) & ((1u << GROUPS) - 1u);
-      if (!edge_of_block(slot0(it), ok)) continue;
+      if (!edge_of_block(slot0(it), on_pages(it, fetch(it)))) continue;
 #pragma unroll 1
       for (int s = slot0(it); s < min(slot0(it) + KT, wk.len); ++s) {
         const long long row_at = cache_row(c, b, h, s);
