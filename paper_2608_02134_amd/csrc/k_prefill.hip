@@ -611,15 +611,34 @@ prefill_join_kernel(CacheView c, AttendArgs a, PreScratch sc) {
 
 static int pre_key_tile(const CacheView& c) { return c.dtype != 0 && c.dh <= 128 ? 64 : 32; }
 
-// Blocks of rows, and the splits of their keys: one while the rows alone fill
-// the chip.
 static int pre_row_blocks(const CacheView& c, int max_new) {
   return static_cast<int>((static_cast<long long>(max_new) * c.hg + kPreRows - 1) / kPreRows);
 }
+
+// Splits of a row block's keys, while the blocks find room on the chip together
+// (512): a block's tiles, one after the other, against a second launch and the
+// parts it reads.  Estimates in us: a tile 1.7 for 64 keys of 128 dims (fp32:
+// 1.9 for 32 of 64), the launch 4, parts 4 MB each.  Measured, us with the splits
+// chosen and with others: 335 tokens (28 query heads on 4 of 128) 16.7 with 1,
+// 20.7 with 2; 1000 tokens 32.5 with 1, 41 with 2; 77 tokens over 4100 slots 27.9
+// with 16, 26.2 with 10, 29.8 with 25; 10 over 2000 14.1 with 15, 19.6 with 5;
+// 200 over 500 (12 on 12 of 96, 2 sequences) 15.1 with 1, 16.7 with 4; fp32 (8 on
+// 2 of 64) 300 tokens 17.0 with 5, 26.6 with 2.
 static int pre_splits(const CacheView& c, int max_new) {
-  const long long most = std::max(1, c.cap / pre_key_tile(c) / 2);
+  const int kt = pre_key_tile(c), tiles = (c.cap + kt - 1) / kt;
   const long long blocks = static_cast<long long>(pre_row_blocks(c, max_new)) * c.hkv * c.n_seq;
-  return static_cast<int>(std::max<long long>(1, std::min<long long>(most, 512 / blocks)));
+  const double tile = (c.dtype == 0 ? 1.9 / (32 * 64) : 1.7 / (64 * 128)) * kt * c.dh;
+  const double part = 8e-6 / 4 * (c.dh + 2) * c.hq * max_new * c.n_seq;
+  int best = 1;
+  double least = tile * tiles;
+  for (int s = 2; s <= tiles / 2 && blocks * s <= 512; ++s) {
+    const double time = tile * tiles / s + 4 + part * s;
+    if (time < least) {
+      least = time;
+      best = s;
+    }
+  }
+  return best;
 }
 
 long long prefill_scratch_bytes(const CacheView& c, int max_new) {
