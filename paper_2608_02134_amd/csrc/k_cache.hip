@@ -123,13 +123,16 @@ __device__ __forceinline__ uint32_t evict_key(float w, bool safe) {
 // lists the slots below the budget that become free and the kept ones at or
 // above it.
 //
-// A pass over weights and positions leaves the upper half of each key (plus
-// one; 0 past the length) in shared memory (KEEP slots; longer caches, KEEP = 0,
-// form them again in every pass).  Histograms of 2048 bins over the halves that
-// there are narrow T's half to a range [lo, hi] that few keys fall into; those
-// are formed again from memory, and T is the one with the right number of larger
+// The keys' upper halves (plus one; 0 past the length) are formed from weights and
+// positions once: a cache of at most 8192 slots keeps them in shared memory, for
+// longer ones a kernel of many blocks before this one leaves them in scratch
+// memory, with histograms of their upper 11 bits (2 x 8 caches of 65536 slots:
+// 5 and 28 us, 39 with all in the one block; at 8192 slots 512 caches take 40 us
+// the short way and 55 the long one, 16 caches 27 either way).  Histograms of 2048 bins over the
+// halves narrow T's half to a range [lo, hi] that few keys fall into; those are
+// formed again from memory, and T is the one with the right number of larger
 // ones.  (More than kEvictList keys with one half: histograms of their lower
-// halves.)
+// halves; comparing 1024 keys with each other would take 22 us.)
 // One block has the work of a whole cache, so what counts is instructions per
 // key, and that the loops over the keys stay loops (unrolled, the kernel waited
 // for its own instructions: 21 us for 4160 slots).  A wave owns a run of
@@ -137,16 +140,68 @@ __device__ __forceinline__ uint32_t evict_key(float w, bool safe) {
 // slot), and one scan per step counts free and moving slots together.  A wave's
 // lists start at its own place, at the first slot of its run; the move kernel
 // strings them together.
-constexpr int kEvictBins = 2048, kEvictList = 1024, kEvictRuns = 16, kEvictHead = 64;
+constexpr int kEvictBins = 2048, kEvictList = 256, kEvictRuns = 16, kEvictHead = 64;
+constexpr int kEvictShort = 8192;                  // slots of a cache whose halves shared memory holds
+constexpr int kEvictSlice = 4096;                  // slots a block of the first kernel takes
+constexpr uint32_t kSafeHalf = 0xFFFFu;            // protected; others are at most 0xFF81
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 
-// Scratch memory: the lengths of the runs' lists, then the lists.
+__device__ __forceinline__ uint32_t evict_half(float w, bool safe) {
+  const uint32_t y = evict_key(w, safe);
+  return y == kSafeKey ? kSafeHalf : (y >> 16) + 1u;
+}
+
+// Scratch memory: the lengths of the runs' lists, then the lists; for long caches
+// the keys' halves and each slice's histogram.
 struct EvictLists {
   int32_t* heads;    // [groups][kEvictHead]: free slots of each run, kept slots above
                      // the budget of each, slots of a run
   int32_t* to;       // [groups][cap]
   int32_t* from;     // [groups][cap]
+  uint16_t* halves;  // [groups][cap]
+  uint16_t* hist;    // [groups][slices][kEvictBins]
 };
+
+__host__ __device__ inline int evict_slices(int slots) { return (slots + kEvictSlice - 1) / kEvictSlice; }
+
+// The halves and histogram of one slice of a long cache.
+__global__ void __launch_bounds__(256)
+evict_halves_kernel(CacheView c, int budget, int sinks, int recent, EvictLists out) {
+  __shared__ int bins[kEvictBins];
+  const int g = blockIdx.x, b = g / c.hkv, first = blockIdx.y * kEvictSlice;
+  const int len = cache_len(c, b);
+  if (len <= budget || first >= len) return;
+  for (int x = threadIdx.x; x < kEvictBins; x += 256) bins[x] = 0;
+  __syncthreads();
+  const long long at = static_cast<long long>(g) * c.cap;
+  const int from_pos = c.seen[b] - recent, end = min(first + kEvictSlice, c.cap);
+  constexpr int kSteps = kEvictSlice / 1024;
+  f32x4_any x[kSteps];
+  i32x4_any p[kSteps];
+#pragma unroll
+  for (int e = 0; e < kSteps; ++e) {
+    const int s = min(first + 1024 * e + 4 * static_cast<int>(threadIdx.x), c.cap - 4);
+    x[e] = *reinterpret_cast<const f32x4_any*>(c.weights + at + s);
+    p[e] = *reinterpret_cast<const i32x4_any*>(c.slot_pos + at + s);
+  }
+#pragma unroll
+  for (int e = 0; e < kSteps; ++e) {
+    const int s = first + 1024 * e + 4 * static_cast<int>(threadIdx.x);
+    if (s >= end) break;
+    uint32_t k[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      k[j] = s + j < len ? evict_half(x[e][j], p[e][j] < sinks || p[e][j] >= from_pos) : 0u;
+      if (k[j]) atomicAdd(&bins[k[j] >> 5], 1);
+    }
+    *reinterpret_cast<uint2*>(out.halves + at + s) = make_uint2(k[0] | (k[1] << 16), k[2] | (k[3] << 16));
+  }
+  __syncthreads();
+  uint32_t* to = reinterpret_cast<uint32_t*>(
+      out.hist + (static_cast<long long>(g) * evict_slices(c.cap) + blockIdx.y) * kEvictBins);
+  for (int x = threadIdx.x; x < kEvictBins / 2; x += 256)
+    to[x] = static_cast<uint32_t>(bins[2 * x]) | (static_cast<uint32_t>(bins[2 * x + 1]) << 16);
+}
 
 template <int THREADS, int KEEP>
 __global__ void __launch_bounds__(THREADS)
@@ -170,11 +225,10 @@ evict_select_kernel(CacheView c, int budget, int sinks, int recent, EvictLists o
   const float* wt = c.weights + static_cast<long long>(g) * c.cap;
   const int32_t* pos = c.slot_pos + static_cast<long long>(g) * c.cap;
   const int from_pos = c.seen[b] - recent;
+  const uint16_t* halves = out.halves + static_cast<long long>(g) * c.cap;
   const int steps = (len + 4 * THREADS - 1) / (4 * THREADS);
   const int s_wave = w * steps * 256, s0 = s_wave + 4 * lane;
-  auto key_of = [&](float weight, int p) { return evict_key(weight, p < sinks || p >= from_pos); };
-  auto again = [&](int s) { return key_of(wt[s], pos[s]); };
-  constexpr uint32_t kSafeHalf = 0xFFFFu;   // protected; others are at most 0xFF81
+  auto again = [&](int s) { return evict_key(wt[s], pos[s] < sinks || pos[s] >= from_pos); };
   // f(the lane's first slot, its four halves) for the wave's steps
   auto from_memory = [&](auto f) {
     constexpr int kFlight = 4;   // steps whose loads are in flight together
@@ -194,30 +248,32 @@ evict_select_kernel(CacheView c, int budget, int sinks, int recent, EvictLists o
         uint32_t k[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const uint32_t y = key_of(x[e][j], p[e][j]);
-          k[j] = s + j >= len ? 0u : y == kSafeKey ? kSafeHalf : (y >> 16) + 1u;
+          k[j] = s + j >= len ? 0u : evict_half(x[e][j], p[e][j] < sinks || p[e][j] >= from_pos);
         }
         f(s, k);
       }
     }
   };
   auto each = [&](auto f) {
-    if constexpr (KEEP > 0) {
-      constexpr int kFlight = 2;
-      for (int i0 = 0; i0 < steps; i0 += kFlight) {
-        uint2 y[kFlight];
+    constexpr int kFlight = KEEP > 0 ? 2 : 8;
+    for (int i0 = 0; i0 < steps; i0 += kFlight) {
+      uint2 y[kFlight];
 #pragma unroll
-        for (int e = 0; e < kFlight; ++e)
+      for (int e = 0; e < kFlight; ++e) {
+        if constexpr (KEEP > 0) {
           y[e] = *reinterpret_cast<const uint2*>(&upper[s0 + 256 * min(i0 + e, steps - 1)]);
-#pragma unroll
-        for (int e = 0; e < kFlight; ++e) {
-          if (i0 + e >= steps) break;
-          const uint32_t k[4] = {y[e].x & 0xFFFFu, y[e].x >> 16, y[e].y & 0xFFFFu, y[e].y >> 16};
-          f(s0 + 256 * (i0 + e), k);
+        } else {
+          const int s = s0 + 256 * (i0 + e);
+          y[e] = *reinterpret_cast<const uint2*>(halves + min(s, c.cap - 4));   // (no branch: all on their way together)
         }
       }
-    } else {
-      from_memory(f);
+#pragma unroll
+      for (int e = 0; e < kFlight; ++e) {
+        if (i0 + e >= steps) break;
+        if (KEEP == 0 && s0 + 256 * (i0 + e) >= len) y[e] = make_uint2(0u, 0u);
+        const uint32_t k[4] = {y[e].x & 0xFFFFu, y[e].x >> 16, y[e].y & 0xFFFFu, y[e].y >> 16};
+        f(s0 + 256 * (i0 + e), k);
+      }
     }
   };
   // one histogram: the bin that the need-th largest of the counted values falls
@@ -251,22 +307,22 @@ evict_select_kernel(CacheView c, int budget, int sinks, int recent, EvictLists o
     return bits > 11 ? bits - 11 : 0;
   };
 
-  // protected slots stay, first of all; the histograms need only span the others
+  // T is the need-th largest key of the `some` keys with halves in [lo, hi]
   uint32_t lo = kSafeHalf, hi = 1u;
-  int safe = 0;
-  from_memory([&](int s, const uint32_t* k) {
-    if constexpr (KEEP > 0)   // (read back by this lane only)
+  int need = budget, some = len;
+  if constexpr (KEEP > 0) {
+    // protected slots stay, first of all; the histograms need only span the others
+    int safe = 0;
+    from_memory([&](int s, const uint32_t* k) {
+      // (read back by this lane only)
       *reinterpret_cast<uint2*>(&upper[s]) = make_uint2(k[0] | (k[1] << 16), k[2] | (k[3] << 16));
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      safe += k[j] == kSafeHalf;
-      lo = k[j] ? min(lo, k[j]) : lo;
-      hi = k[j] != kSafeHalf ? max(hi, k[j]) : hi;
-    }
-  });
-  int need = budget;         // T is the need-th largest key of the `some` keys with halves in [lo, hi]
-  int some = len;
-  {
+      for (int j = 0; j < 4; ++j) {
+        safe += k[j] == kSafeHalf;
+        lo = k[j] ? min(lo, k[j]) : lo;
+        hi = k[j] != kSafeHalf ? max(hi, k[j]) : hi;
+      }
+    });
     const float l = wave_min(static_cast<float>(lo)), h = wave_max(static_cast<float>(hi));   // (exact)
     if (lane == 0) { range[0][w] = l; range[1][w] = h; }
     int all;
@@ -283,6 +339,30 @@ evict_select_kernel(CacheView c, int budget, int sinks, int recent, EvictLists o
       need -= all;
       some -= all;
     }
+  } else {
+    int n[PER] = {};
+    static_assert(PER == 2, "two bins a thread");
+    const uint32_t* hist = reinterpret_cast<const uint32_t*>(
+        out.hist + static_cast<long long>(g) * evict_slices(c.cap) * kEvictBins);
+    const int slices = evict_slices(len);
+#pragma unroll 8
+    for (int u = 0; u < slices; ++u) {
+      const uint32_t y = hist[static_cast<long long>(u) * (kEvictBins / 2) + threadIdx.x];
+      n[0] += y & 0xFFFFu;
+      n[1] += y >> 16;
+    }
+    bins[2 * threadIdx.x] = n[0];
+    bins[2 * threadIdx.x + 1] = n[1];
+    find_bin(need);
+    if (found[0] == static_cast<int>(kSafeHalf >> 5)) {   // (more protected slots than the budget: positions given twice)
+      hi = kSafeHalf;
+    } else {
+      lo = max(static_cast<uint32_t>(found[0]) << 5, 1u);
+      hi = (static_cast<uint32_t>(found[0]) << 5) + 31u;
+    }
+    need -= found[1];
+    some = found[2];
+    __syncthreads();
   }
   while (lo < hi && need < some && some > kEvictList) {
     const int shift = width(hi - lo);
@@ -511,27 +591,28 @@ evict_move_kernel(CacheView c, int budget, EvictLists in, int chunks) {
 }
 
 long long evict_scratch_bytes(const CacheView& c) {
-  return 4ll * c.n_seq * c.hkv * (kEvictHead + 2ll * c.cap);
+  const long long groups = static_cast<long long>(c.n_seq) * c.hkv;
+  const long long lists = 4 * groups * (kEvictHead + 2ll * c.cap);
+  return c.cap <= kEvictShort ? lists : lists + 2 * groups * (c.cap + static_cast<long long>(evict_slices(c.cap)) * kEvictBins);
 }
 
 hipError_t launch_cache_evict(const CacheView& c, int budget, int sinks, int recent, void* scratch, hipStream_t st) {
   const int esz = c.dtype == 0 ? 4 : 2, chunks = c.dh * esz / 16;
   const long long groups = static_cast<long long>(c.n_seq) * c.hkv;
-  EvictLists lists;
+  EvictLists lists;   // (each part begins at a multiple of 16 bytes: cap is one of 16 slots)
   lists.heads = static_cast<int32_t*>(scratch);
   lists.to = lists.heads + groups * kEvictHead;
   lists.from = lists.to + groups * c.cap;
-#define GMC_EVICT(THREADS, KEEP)                                                                                 \
-  hipLaunchKernelGGL((evict_select_kernel<THREADS, KEEP>), dim3(groups), dim3(THREADS), 0, st, c, budget, sinks, recent, \
-                     lists)
-  if (c.cap <= 8192) {
-    GMC_EVICT(256, 8192);
-  } else if (c.cap <= 65536) {
-    GMC_EVICT(1024, 65536);
+  lists.halves = reinterpret_cast<uint16_t*>(lists.from + groups * c.cap);
+  lists.hist = lists.halves + groups * c.cap;
+  if (c.cap <= kEvictShort) {
+    hipLaunchKernelGGL((evict_select_kernel<256, kEvictShort>), dim3(groups), dim3(256), 0, st, c, budget, sinks, recent,
+                       lists);
   } else {
-    GMC_EVICT(1024, 0);
+    hipLaunchKernelGGL(evict_halves_kernel, dim3(groups, evict_slices(c.cap)), dim3(256), 0, st, c, budget, sinks, recent,
+                       lists);
+    hipLaunchKernelGGL((evict_select_kernel<1024, 0>), dim3(groups), dim3(1024), 0, st, c, budget, sinks, recent, lists);
   }
-#undef GMC_EVICT
   const long long total = static_cast<long long>(std::min(c.cap - budget, budget)) * chunks;   // pieces that can move
   const int gy =
       static_cast<int>(std::max<long long>(1, std::min<long long>((total + 256 * kMoveDepth - 1) / (256 * kMoveDepth), 1024)));

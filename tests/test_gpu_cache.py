@@ -687,3 +687,24 @@ def test_wrapper_refusals_on_the_device():
         with pytest.raises(RuntimeError, match=what):
             call()
     assert dev.lens.tolist() == [30, 40]
+
+
+@pytest.mark.parametrize("kind", ["odd", "one_value", "protected"])
+def test_evict_of_long_caches_of_unlike_lengths(kind):
+    """Sequences below the budget, of one slice and of many in one call; infinities
+    and NaN; one weight for all; more protected rows than the budget."""
+    _say(f"evict unlike {kind}")
+    rng = np.random.default_rng(38)
+    c = C.make(rng, dtype="bf16", hq=4, hkv=2, dh=32, page=16, lens=[100, 4097, 12300, 3000, 0], slots=12304,
+               positions=True, weights=True)
+    w = c["weights"]
+    if kind == "odd":
+        w[:] = rng.choice([0.0, -0.0, np.inf, -np.inf, np.nan, -1.0, 1e-40, 3.0], w.shape).astype(np.float32)
+    if kind == "one_value":
+        w[:] = 0.125
+    if kind == "protected":
+        c["slot_pos"][2, 1, ::2] = 0
+    dev = C.on_gpu(c)
+    dev.evict(3000, sinks=2, recent=900)
+    O.evict(c, 3000, 2, 900)
+    _compare_caches(c, dev)
