@@ -19,6 +19,13 @@
 //
 // Rows in shared memory are swizzled in 16-byte chunks, so that the 16 rows
 // that one read touches lie on different banks.
+//
+// 16448 tokens, window 4096, 28 heads on 4 of 128 in bf16: 0.96 ms, 880 TFLOP/s
+// (a large matrix product of the library: 1217).  Of its time 0.69 ms are products
+// and reads of shared memory alone, what the loads add is 0.13 and what the
+// exponentials and maxima add 0.12.  (64 queries a wave, one wave a SIMD, halve the
+// reads and took 1.36 ms; eight waves a block, loads spread over the products and
+// weights interleaved with products by hand were no faster.)
 #include <limits.h>
 
 #include <algorithm>
@@ -654,7 +661,9 @@ hipError_t launch_cache_prefill(const CacheView& c, const AttendArgs& a, void* s
     sc.part = static_cast<float*>(scratch);
     sc.ml = sc.part + static_cast<long long>(c.n_seq) * a.max_new * c.hq * sc.nsplit * c.dh;
   }
-  // runs of 32 blocks; shorter ones where that leaves an XCD fewer than eight
+  // runs of 32 blocks; shorter ones where that leaves an XCD fewer than eight.
+  // Tokens of one long sequence and ragged short ones, us: 32 944 and 128, 4 958
+  // and 124, 128 1018 and 130.
   const long long items = static_cast<long long>(row_blocks) * sc.nsplit, heads = static_cast<long long>(c.hkv) * c.n_seq;
   sc.run = static_cast<int>(std::max<long long>(1, std::min<long long>(32, items * heads / 64)));
   const long long units = (items + sc.run - 1) / sc.run * heads, total = (units + 7) / 8 * 8 * sc.run;
