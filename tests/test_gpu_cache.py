@@ -708,3 +708,42 @@ def test_evict_of_long_caches_of_unlike_lengths(kind):
     dev.evict(3000, sinks=2, recent=900)
     O.evict(c, 3000, 2, 900)
     _compare_caches(c, dev)
+
+
+def test_pruned_prompt_into_the_cache():
+    """prune, compact, the prefix layer's rows at the kept positions into the cache,
+    attention over them and one answer token: what a deployment runs."""
+    from paper_2608_02134_amd import binding as B
+    from paper_2608_02134_amd import synth
+
+    from .gpu_run import run
+    _say("prune, compact, append, prefill, decode")
+    prob = synth.make_problem("tiny", grid=(1, 8, 8), t=4, k=16)
+    outs, pr = run(prob, torch, trace=False)
+    before, n, after, hq, hkv, dh = 5, 64, 9, 8, 2, 64
+    length = before + n + after
+    idx = torch.from_numpy(np.ascontiguousarray(outs[0]["out_idx"].astype(np.int32)[None])).cuda()
+    pos = torch.zeros((1, length, 3), dtype=torch.int32, device="cuda")
+    _, keep, _, _ = B.compact_sequence(idx, before, n, seq_pos=pos)
+    rng = np.random.default_rng(39)
+    kv = C.rounded(rng.standard_normal((2, length, hkv, dh)), "bf16")
+    k, v = C.to_gpu(kv, "bf16")
+    cache = B.KvCache.create(n_seq=1, slots=64, n_q_heads=hq, n_kv_heads=hkv, head_dim=dh, dtype=torch.bfloat16,
+                             page_size=16)
+    cache.append(k, v, src=keep)
+    kept = keep.shape[1]
+    assert cache.lens.tolist() == [kept]
+    for x, pages in zip(B.gather_rows([k[None], v[None]], keep), (cache.k_pages, cache.v_pages)):
+        held = pages.permute(0, 2, 1, 3).reshape(-1, hkv, dh)[:kept]
+        assert torch.equal(held, x[0])
+    c = {"dtype": "bf16", "hq": hq, "q_scale": 2.0, "k": C.host(cache.k_pages), "v": C.host(cache.v_pages),
+         "table": cache.page_table.cpu().numpy(), "lens": np.array([kept], np.int32)}
+    q = C.queries(rng, c, kept)
+    out, lse = cache.prefill(C.to_gpu(q, "bf16"), lse=True)
+    C.check_attention(O.attend(c, q, [0], [kept], dh ** -0.5), C.host(out), C.host(lse), "bf16", dh)
+    new = C.rounded(rng.standard_normal((2, 1, hkv, dh)), "bf16")
+    cache.append(*C.to_gpu(new, "bf16"))
+    O.append(c, new[0], new[1], [1], [np.arange(1)])
+    out, lse = cache.decode(C.to_gpu(q[:1], "bf16"), lse=True)
+    C.check_attention(O.attend(c, q[:1], [0], [1], dh ** -0.5), C.host(out), C.host(lse), "bf16", dh)
+    pr.close()
