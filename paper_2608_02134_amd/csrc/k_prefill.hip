@@ -348,7 +348,8 @@ prefill_kernel(CacheView c, AttendArgs a, PreScratch sc, int row_blocks) {
     }
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) settle(x[kb]);
-    if (!all || pos || (a.window && s0 < a.sinks)) {
+    const bool before = a.window && s0 + KT - 1 <= wt_min - a.window;   // the windows of all queries
+    if (!all || pos || (a.window && s0 < a.sinks && !before)) {
       const int win = a.window ? a.window : INT_MAX;
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
@@ -370,9 +371,11 @@ prefill_kernel(CacheView c, AttendArgs a, PreScratch sc, int row_blocks) {
         }
     } else if (s0 + KT - 1 > wt_min || (a.window && wt_max - s0 >= a.window)) {
       // the slots that a query sees are one run: of `span` + 1 from `lo` on (none:
-      // t < 0, then lo is past the tile)
-      const int lo = t < 0 ? INT_MAX : a.window && t >= a.window ? t - a.window + 1 : 0;
-      const unsigned span = t < 0 ? 0u : static_cast<unsigned>(t - lo);
+      // lo is past the tile)
+      int lo = a.window && t >= a.window ? t - a.window + 1 : 0, end = t;
+      if (before) { lo = 0; end = a.sinks - 1; }
+      if (end < 0) { lo = INT_MAX; end = INT_MAX; }
+      const unsigned span = static_cast<unsigned>(end - lo);
       const unsigned at = static_cast<unsigned>(s0 + 4 * half) - static_cast<unsigned>(lo);
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
