@@ -20,7 +20,7 @@
 // Rows in shared memory are swizzled in 16-byte chunks, so that the 16 rows
 // that one read touches lie on different banks.
 //
-// 16448 tokens, window 4096, 28 heads on 4 of 128 in bf16: 0.96 ms, 880 TFLOP/s
+// 16448 tokens, window 4096, 28 heads on 4 of 128 in bf16: 0.95 ms, 890 TFLOP/s
 // (a large matrix product of the library: 1217).  Of its time 0.69 ms are products
 // and reads of shared memory alone, what the loads add is 0.13 and what the
 // exponentials and maxima add 0.12.  (64 queries a wave, one wave a SIMD, halve the
@@ -180,7 +180,7 @@ prefill_kernel(CacheView c, AttendArgs a, PreScratch sc, int row_blocks) {
     const bool on = slot0(it) + 16 * (lane & (GROUPS - 1)) < wk.len && ids >= 0 && ids < c.n_pages;
     return static_cast<unsigned>(__ballot(on)) & ((1u << GROUPS) - 1u);
   };
-  int ids0 = fetch(it0), ids1 = fetch(it0 + 1);
+  const int ids0 = fetch(it0), ids1 = fetch(it0 + 1);
 
   uint4 q[NS];
   {
@@ -348,7 +348,8 @@ prefill_kernel(CacheView c, AttendArgs a, PreScratch sc, int row_blocks) {
     }
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) settle(x[kb]);
-    const bool before = a.window && s0 + KT - 1 <= wt_min - a.window;   // the windows of all queries
+    // (compared first: t may be negative and the window as large as an integer)
+    const bool before = a.window && wt_min >= a.window && s0 + KT - 1 <= wt_min - a.window;   // the windows of all queries
     if (!all || pos || (a.window && s0 < a.sinks && !before)) {
       const int win = a.window ? a.window : INT_MAX;
 #pragma unroll

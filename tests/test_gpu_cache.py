@@ -747,3 +747,15 @@ def test_pruned_prompt_into_the_cache():
     out, lse = cache.decode(C.to_gpu(q[:1], "bf16"), lse=True)
     C.check_attention(O.attend(c, q[:1], [0], [1], dh ** -0.5), C.host(out), C.host(lse), "bf16", dh)
     pr.close()
+
+
+@pytest.mark.parametrize("window,sinks", [(2 ** 31 - 1, 3), (2 ** 31 - 1, 2 ** 31 - 1), (70, 2 ** 31 - 1), (1, 64), (1, 0)])
+@pytest.mark.parametrize("positions", [False, True])
+def test_windows_and_first_tokens_of_any_size(window, sinks, positions):
+    """Also with queries whose own slot lies before the cache's first."""
+    _say(f"window {window} sinks {sinks} positions {positions}")
+    for dtype in ("bf16", "f32"):
+        rng = np.random.default_rng(40)
+        c = C.make(rng, dtype=dtype, hq=4, hkv=2, dh=64, page=16, lens=[5, 300, 64], slots=304, positions=positions)
+        _prefill(rng, c, [9, 200, 64], window, sinks)
+        _decode(rng, c, window, sinks)
