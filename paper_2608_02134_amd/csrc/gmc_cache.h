@@ -11,6 +11,10 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#ifdef __HIPCC__
+#include "gmc_device.h"
+#endif
+
 namespace gmc {
 
 constexpr int kCacheMaxHeads = 256;   // GMC_CACHE_MAX_HEADS
@@ -73,6 +77,21 @@ __device__ __forceinline__ void new_rows(const int32_t* starts, int max_new, lon
     *first = lo;
     *n = static_cast<int>(min(max(hi - lo, 0ll), static_cast<long long>(max_new)));
   }
+}
+
+// The maximum and sum (both base 2) of a row over its splits.
+__device__ __forceinline__ void join_stats(const float* ml, int ns, float* m_out, float* l_out) {
+  const int lane = threadIdx.x & 63;
+  float m = -INFINITY, l = 0.f;
+  for (int s = lane; s < ns; s += 64) {
+    const float2 y = *reinterpret_cast<const float2*>(ml + 2 * s);
+    const float mn = fmaxf(m, y.x), base = mn == -INFINITY ? 0.f : mn;
+    l = l * __builtin_amdgcn_exp2f(m - base) + y.y * __builtin_amdgcn_exp2f(y.x - base);
+    m = mn;
+  }
+  const float mw = wave_max(m), base = mw == -INFINITY ? 0.f : mw;
+  *l_out = wave_sum(l * __builtin_amdgcn_exp2f(m - base));
+  *m_out = mw;
 }
 #endif
 

@@ -341,21 +341,6 @@ decode_split_kernel(CacheView c, AttendArgs a, DecodeScratch sc, int qtiles) {
   if (a.lse && g == 0) a.lse[row] = lb == 0.f ? -INFINITY : (mb + __builtin_amdgcn_logf(lb)) * kLn2;
 }
 
-// The maximum and sum (both base 2) of a row over its splits.
-__device__ __forceinline__ void join_stats(const float* ml, int ns, float* m_out, float* l_out) {
-  const int lane = threadIdx.x & 63;
-  float m = -INFINITY, l = 0.f;
-  for (int s = lane; s < ns; s += 64) {
-    const float2 y = *reinterpret_cast<const float2*>(ml + 2 * s);
-    const float mn = fmaxf(m, y.x), base = mn == -INFINITY ? 0.f : mn;
-    l = l * __builtin_amdgcn_exp2f(m - base) + y.y * __builtin_amdgcn_exp2f(y.x - base);
-    m = mn;
-  }
-  const float mw = wave_max(m), base = mw == -INFINITY ? 0.f : mw;
-  *l_out = wave_sum(l * __builtin_amdgcn_exp2f(m - base));
-  *m_out = mw;
-}
-
 // Joins a sequence's splits.  blockIdx.x < hg: output and lse of one query
 // head of the kv head, its splits shared by the block's waves; above: the
 // weights of one run of 1024 slots, for which each wave first takes the lse of

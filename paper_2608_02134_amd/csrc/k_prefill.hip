@@ -20,7 +20,7 @@
 // Rows in shared memory are swizzled in 16-byte chunks, so that the 16 rows
 // that one read touches lie on different banks.
 //
-// 16448 tokens, window 4096, 28 heads on 4 of 128 in bf16: 0.95 ms, 890 TFLOP/s
+// 16448 tokens, window 4096, 28 heads on 4 of 128 in bf16: 0.94 to 1.01 ms, 840 to 900 TFLOP/s
 // (a large matrix product of the library: 1217).  Of its time 0.69 ms are products
 // and reads of shared memory alone, what the loads add is 0.13 and what the
 // exponentials and maxima add 0.12.  (64 queries a wave, one wave a SIMD, halve the
@@ -568,7 +568,11 @@ prefill_kernel(CacheView c, AttendArgs a, PreScratch sc, int row_blocks) {
   if (a.lse && half == 0) a.lse[out_row] = l == 0.f ? -INFINITY : (mc + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
-// Joins the splits: one wave per row and head, four elements a lane.
+// Joins the splits: one wave per row and head, four elements a lane; lanes that a
+// row leaves over take other splits (77 tokens of 3 requests, 8 heads of 64, 28
+// splits: 5.2 us, 8.4 with 16 lanes at work).  Up to 8 splits every lane takes all
+// statistics itself: 4 requests of 77 tokens, 6 splits, 49.5 us for both kernels,
+// 51.3 with the exchange; 16 tokens, 64 splits, 37 with it.
 template <typename T>
 __global__ void __launch_bounds__(256)
 prefill_join_kernel(CacheView c, AttendArgs a, PreScratch sc) {
@@ -578,39 +582,53 @@ prefill_join_kernel(CacheView c, AttendArgs a, PreScratch sc) {
   new_rows(a.starts, a.max_new, a.rows, b, &first, &n);
   if (i >= n) return;
   const long long row = (first + i) * c.hq + hq, part_row = (static_cast<long long>(b) * a.max_new + i) * c.hq + hq;
-  const float* ml = sc.ml + part_row * sc.nsplit * 2;
-  const float* part = sc.part + part_row * sc.nsplit * c.dh + 4 * lane;
-  const bool mine = 4 * lane < c.dh;
+  const float2* ml = reinterpret_cast<const float2*>(sc.ml) + part_row * sc.nsplit;
+  const int per = c.dh / 4, groups = 64 / per, g = lane / per;   // lanes of a row, rows at once
+  const float* part = sc.part + part_row * sc.nsplit * c.dh + 4 * (lane - g * per);
   constexpr int kFlight = 8;
+  floatx4 x[kFlight];
+  float2 y[kFlight];
+  auto load = [&](int s0) {
+#pragma unroll
+    for (int e = 0; e < kFlight; ++e) {
+      const int s = min(s0 + e * groups, sc.nsplit - 1);
+      y[e] = ml[s];
+      x[e] = *reinterpret_cast<const floatx4*>(part + static_cast<long long>(s) * c.dh);
+    }
+  };
+  load(g);                     // (on its way while the statistics are taken)
   float m = -INFINITY, l = 0.f;
-  floatx4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int s0 = 0; s0 < sc.nsplit; s0 += kFlight) {
-    floatx4 x[kFlight];
-    float mi[kFlight], li[kFlight];
+  if (sc.nsplit <= kFlight) {  // every lane takes them all: no exchange between lanes
+    float2 z[kFlight];
 #pragma unroll
-    for (int e = 0; e < kFlight; ++e) {
-      const int s = min(s0 + e, sc.nsplit - 1);
-      mi[e] = s0 + e < sc.nsplit ? ml[2 * s] : -INFINITY;
-      li[e] = s0 + e < sc.nsplit ? ml[2 * s + 1] : 0.f;
-      x[e] = floatx4{0.f, 0.f, 0.f, 0.f};
-      if (mine && (mi[e] != -INFINITY || li[e] != 0.f)) x[e] = *reinterpret_cast<const floatx4*>(part + static_cast<long long>(s) * c.dh);
-    }
-    float mn = m;
+    for (int e = 0; e < kFlight; ++e) z[e] = e < sc.nsplit ? ml[e] : make_float2(-INFINITY, 0.f);
 #pragma unroll
-    for (int e = 0; e < kFlight; ++e) mn = fmaxf(mn, mi[e]);
-    const float base = mn == -INFINITY ? 0.f : mn, f = __builtin_amdgcn_exp2f(m - base);
-    l *= f;
-    o *= f;
+    for (int e = 0; e < kFlight; ++e) m = fmaxf(m, z[e].x);
 #pragma unroll
-    for (int e = 0; e < kFlight; ++e) {
-      const float g = __builtin_amdgcn_exp2f(mi[e] - base);
-      l += li[e] * g;
-#pragma unroll
-      for (int u = 0; u < 4; ++u) o[u] += x[e][u] * g;
-    }
-    m = mn;
+    for (int e = 0; e < kFlight; ++e) l += z[e].y * __builtin_amdgcn_exp2f(z[e].x - (m == -INFINITY ? 0.f : m));
+  } else {
+    join_stats(reinterpret_cast<const float*>(ml), sc.nsplit, &m, &l);
   }
-  if (mine) {
+  const float base = m == -INFINITY ? 0.f : m;
+  floatx4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int s0 = g; s0 < sc.nsplit; s0 += groups * kFlight) {
+    if (s0 > g) load(s0);
+#pragma unroll
+    for (int e = 0; e < kFlight; ++e) {
+      // (a split without a part has written its statistics only)
+      if (s0 + e * groups >= sc.nsplit || (y[e].x == -INFINITY && y[e].y == 0.f)) continue;
+      const float f = __builtin_amdgcn_exp2f(y[e].x - base);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) o[u] += f * x[e][u];
+    }
+  }
+  for (int k = 1; k < groups; ++k)
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const float other = __shfl(o[u], (lane + k * per) & 63);
+      if (g == 0) o[u] += other;
+    }
+  if (g == 0) {
     T* to = static_cast<T*>(a.out) + row * c.dh + 4 * lane;
     const float inv = 1.f / l;
 #pragma unroll
