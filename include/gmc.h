@@ -565,7 +565,7 @@ typedef struct gmc_cache {
  * i and its weight 0; then lens[b] and seen[b] grow by n_b.
  *   k, v    rows of n_kv_heads * head_dim elements, k_stride and v_stride
  *           elements apart (slices of a wider projection); 16-byte aligned,
- *           strides a multiple of 16 bytes
+ *           strides a multiple of 16 bytes and at most 2^24 elements
  *   rows    rows that k and v hold
  *   starts  [n_seq + 1] int32: sequence b's rows are [starts[b], starts[b + 1])
  *           of k and v, at most max_new of them are taken (0 is fine); NULL:
@@ -593,7 +593,7 @@ int gmc_cache_append(const gmc_cache* cache, const void* k, const void* v, int64
  * lse = -inf.  Nothing that a query does not see changes its result, not even
  * infinities and NaN.
  *   q       rows of n_q_heads * head_dim elements, q_stride elements apart
- *           (16-byte aligned, stride a multiple of 16 bytes)
+ *           (16-byte aligned, stride as above)
  *   rows    rows that q and out hold
  *   starts  [n_seq + 1] int32: sequence b's rows of q; at most max_new of them
  *           are computed; NULL: max_new each.  Rows of out that belong to no

@@ -53,7 +53,7 @@ size_t elem(const CacheView& c) { return c.dtype == GMC_F32 ? 4 : 2; }
 int check_rows(const char* fn, const char* name, const CacheView& c, const void* p, int64_t stride, int64_t width) {
   if (!p) return set_error(GMC_ERR_ARG, "%s: %s is NULL", fn, name);
   if (misaligned(p, 16) || stride < width || stride * elem(c) % 16 != 0 || stride > (1ll << 24))
-    return set_error(GMC_ERR_ARG, "%s: %s must be 16-byte aligned with rows a multiple of 16 bytes and at least %lld "
+    return set_error(GMC_ERR_ARG, "%s: %s must be 16-byte aligned with rows a multiple of 16 bytes and %lld to 2^24 "
                      "elements apart (stride=%lld)", fn, name, ll(width), ll(stride));
   return GMC_OK;
 }

@@ -183,3 +183,10 @@ def test_prefill_of_more_blocks_than_a_grid_holds():
     _refused(call(_cache(n_seq=1, n_q_heads=256, n_kv_heads=1, head_dim=32, **big), 1 << 24), "2^23 blocks")
     _refused(call(_cache(n_seq=65535, n_q_heads=256, n_kv_heads=256, head_dim=32, **big), 1), "2^23 blocks")
     _refused(call(_cache(n_seq=3000, n_q_heads=8, n_kv_heads=2, head_dim=64, **big), 100000), "2^23 blocks")
+
+
+def test_rows_too_far_apart():
+    c = _cache()
+    _refused(B.gmc_cache_append(c, P, P, (1 << 24) + 8, 512, 2, None, None, 1), "2^24")
+    _refused(B.gmc_cache_prefill(c, P, (1 << 24) + 8, 2, None, 1, 0.1, 0, 0, P, None, P, 1 << 40), "2^24")
+    _refused(B.gmc_cache_decode(c, P, (1 << 24) + 8, 0.1, 0, 0, 0, P, None, P, 1 << 40), "2^24")
