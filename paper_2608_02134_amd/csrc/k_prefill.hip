@@ -293,9 +293,13 @@ prefill_kernel(CacheView c, AttendArgs a, PreScratch sc, int row_blocks) {
   auto compute = [&](int it, unsigned ok, shared_u8* ks, shared_u8* vs, shared_u8* ps) GMC_INLINE {
     const int s0 = slot0(it);
     if (care && edge_of_block(s0, ok)) {
+      // (bf16 tiles of 160 and 224 dims have 640 and 896 chunks: the last round is
+      // for half of the threads)
+      constexpr int kChunks = KT * CPR, kThreads = 64 * kPreWaves;
 #pragma unroll 1
-      for (int x = 0; x < KT * CPR / (64 * kPreWaves); ++x) {
-        shared_u8* at = vs + 16 * (64 * kPreWaves * x + static_cast<int>(threadIdx.x));
+      for (int x = 0; x < (kChunks + kThreads - 1) / kThreads; ++x) {
+        if (kChunks % kThreads != 0 && kThreads * x + static_cast<int>(threadIdx.x) >= kChunks) break;
+        shared_u8* at = vs + 16 * (kThreads * x + static_cast<int>(threadIdx.x));
         u32x4 y = ld_shared<u32x4>(at);
         if (clean(y)) *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(at) = y;
       }

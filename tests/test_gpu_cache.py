@@ -759,3 +759,44 @@ def test_windows_and_first_tokens_of_any_size(window, sinks, positions):
         c = C.make(rng, dtype=dtype, hq=4, hkv=2, dh=64, page=16, lens=[5, 300, 64], slots=304, positions=positions)
         _prefill(rng, c, [9, 200, 64], window, sinks)
         _decode(rng, c, window, sinks)
+
+
+# --- infinities and NaN at every head size ------------------------------------------------
+def _bits(t):
+    return t.view(torch.int16 if t.dtype == torch.bfloat16 else torch.int32)
+
+
+@pytest.mark.parametrize("dh", [32, 64, 96, 128, 160, 192, 224, 256])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("held,new,window", [(200, 200, (0, 0)), (200, 200, (20, 2)), (607, 37, (0, 0)), (607, 37, (300, 2))],
+                         ids=str)
+def test_unseen_infinities_at_every_head_size(dh, dtype, held, new, window):
+    """A value row of infinities or NaN at the first, a late and the last row of a
+    key tile (of 32 or 64), in the first, the last or all dims: queries that do
+    not see it keep their bits, the others those of the other dims.  A whole
+    prompt, and a few tokens over a longer cache (keys split and joined)."""
+    _say(f"unseen at {dh} {dtype} {held} {new} {window}")
+    rng = np.random.default_rng(dh)
+    c = C.make(rng, dtype=dtype, hq=6, hkv=2, dh=dh, page=16, lens=[held], slots=608)
+    dev, q = C.on_gpu(c), C.to_gpu(C.queries(rng, c, new), dtype)
+    clean, clean_lse = dev.prefill(q, window=window[0], sinks=window[1], lse=True)
+    assert torch.isfinite(clean).all()
+    t = np.arange(held - new, held)
+    edge = held - new if new < held else 96       # a tile that some queries see in part
+    slots = [edge // 32 * 32 + x for x in (0, 26, 30, 31, 32)] + [held - 1]
+    if window[0] and new < held:
+        slots += [t[0] - window[0] + 1 + x for x in (0, 16, 17)]      # 271, 287 and 288: the windows begin here
+    for i, slot in enumerate(slots):
+        p, r = O.row_of(c, 0, 0, slot)
+        dims = [slice(0, 8), slice(dh - 8, dh), slice(0, dh)][i % 3]
+        keep = dev.v_pages[p, :, r].clone()
+        dev.v_pages[p, :, r, dims] = (np.nan, np.inf, -np.inf)[i // 2 % 3]
+        out, lse = dev.prefill(q, window=window[0], sinks=window[1], lse=True)
+        dev.v_pages[p, :, r] = keep
+        sees = torch.from_numpy((t >= slot) & ((window[0] == 0) | (t - slot < window[0]))).cuda()
+        assert torch.equal(lse, clean_lse), slot
+        assert torch.equal(_bits(out[~sees]), _bits(clean[~sees])), (slot, dims)
+        other = torch.ones(dh, dtype=torch.bool, device="cuda")
+        other[dims] = False
+        assert torch.equal(_bits(out[..., other]), _bits(clean[..., other])), (slot, dims)
+        assert not torch.isfinite(out[sees][..., ~other]).any(), (slot, dims)
