@@ -424,7 +424,10 @@ decode_join_kernel(CacheView c, AttendArgs a, DecodeScratch sc, int tk) {
     for (int e = 0; e < kFlight; ++e) {
       if (head + e >= c.hg) break;
 #pragma unroll
-      for (int u = 0; u < 4; ++u) add[u] += __builtin_amdgcn_exp2f(x[e][u] - lse2[head + e]);
+      for (int u = 0; u < 4; ++u) {   // (a slot that is not seen gains nothing, also where the lse is NaN)
+        const float p = __builtin_amdgcn_exp2f(x[e][u] - lse2[head + e]);
+        add[u] += x[e][u] == -INFINITY ? 0.f : p;
+      }
     }
   }
   float* to = c.weights + (static_cast<long long>(b) * c.hkv + h) * c.cap + s;

@@ -800,3 +800,37 @@ def test_unseen_infinities_at_every_head_size(dh, dtype, held, new, window):
         other[dims] = False
         assert torch.equal(_bits(out[..., other]), _bits(clean[..., other])), (slot, dims)
         assert not torch.isfinite(out[sees][..., ~other]).any(), (slot, dims)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("slots", [48, 1600])
+def test_weights_of_unseen_slots_stay_where_a_seen_key_is_nan(dtype, slots):
+    """The query's own weights are NaN then; slots outside the window, on pages that
+    are none and in other sequences gain nothing."""
+    _say(f"weights beside NaN {dtype} {slots}")
+    rng = np.random.default_rng(41)
+    n = slots - 5
+    c = C.make(rng, dtype=dtype, hq=6, hkv=2, dh=64, page=16, lens=[n, n, 20], slots=slots, weights=True)
+    window, sinks = 21, 3
+    p, r = O.row_of(c, 0, 1, n - 2)
+    c["k"][p, 1, r] = np.nan                     # kv head 1 of sequence 0, seen
+    p, r = O.row_of(c, 1, 0, n - 24)
+    c["k"][p, :, r] = np.nan                     # sequence 1, outside the window
+    c["table"][0, (n - 20) // 16] = -1           # some of the window's slots
+    q = C.queries(rng, c, 3)
+    dev = C.on_gpu(c)
+    _, lse = dev.decode(C.to_gpu(q, dtype), window=window, sinks=sinks, accumulate=True, lse=True)
+    ref = O.attend(c, q, [0, 1, 2], [1, 1, 1], 0.125, window, sinks)
+    got, seen = C.host(dev.weights), np.zeros(c["weights"].shape, bool)
+    for b, m in enumerate(c["lens"]):
+        s = np.arange(m)
+        held = np.array([O.row_of(c, b, 0, x) is not None for x in s])
+        seen[b, :, :m] = held & ((m - 1 - s < window) | (s < sinks))
+    assert np.array_equal(got[~seen], c["weights"][~seen])
+    assert np.isnan(got[0, 1][seen[0, 1]]).all() and np.isnan(C.host(lse)[0, 3:]).all()
+    ok = np.ones(3 * 2, bool)
+    ok[1] = False                                # (every other sequence and kv head)
+    rel = C.weight_error(ref, 64).reshape(3, 2, -1).max(2)
+    want = c["weights"] + ref["probs"]
+    for b, h in np.argwhere(ok.reshape(3, 2)):
+        assert (np.abs(got[b, h] - want[b, h]) <= ref["probs"][b, h] * rel[b, h] + 40 * C.U32 * np.abs(want[b, h])).all(), (b, h)
