@@ -165,8 +165,9 @@ prefill_kernel(CacheView c, AttendArgs a, PreScratch sc, int row_blocks) {
   if (pos) pos += at;
   const int mine = pos && t >= 0 ? pos[t] : t;
   // exp2(scale log2(e) s): a negative scale goes to the queries' sign, and a
-  // scale of zero to one that does not turn a hidden key's -inf into NaN
-  const float cs = fmaxf(fabsf(a.scale) * 1.4426950408889634f, 1e-30f);
+  // scale of zero to the least one that does not turn a hidden key's -inf into
+  // NaN (the largest product then makes a logit of 5e-7)
+  const float cs = fmaxf(fabsf(a.scale) * 1.4426950408889634f, 0x1p-149f);
 
   const int32_t* table = c.table + static_cast<long long>(b) * c.max_pages;
   auto slot0 = [&](int it) GMC_INLINE { return (it < wk.sink_tiles ? it : it + wk.skip) * KT; };
@@ -194,7 +195,7 @@ prefill_kernel(CacheView c, AttendArgs a, PreScratch sc, int row_blocks) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[n][i] = 0.f;
   float m = -INFINITY, l = 0.f;
-  const float slack = 8.f / cs;
+  const float slack = fminf(8.f / cs, 0x1p126f);   // (not infinite: the first maximum is above -inf + slack)
 
   // Offsets of a lane's reads.  With a power of two of chunks to a row they are
   // exclusive ors of one offset each with constants, and are formed where they

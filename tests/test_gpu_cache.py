@@ -834,3 +834,25 @@ def test_weights_of_unseen_slots_stay_where_a_seen_key_is_nan(dtype, slots):
     want = c["weights"] + ref["probs"]
     for b, h in np.argwhere(ok.reshape(3, 2)):
         assert (np.abs(got[b, h] - want[b, h]) <= ref["probs"][b, h] * rel[b, h] + 40 * C.U32 * np.abs(want[b, h])).all(), (b, h)
+
+
+@pytest.mark.parametrize("scale", [0.0, 2e-32, -2e-32, 1e-44])
+def test_scales_far_below_one(scale):
+    """Products far above one: only the scale makes logits of them, and a scale of
+    zero still weighs every visible key alike."""
+    _say(f"scale {scale}")
+    for dtype in ("bf16", "f32"):
+        rng = np.random.default_rng(42)
+        c = C.make(rng, dtype=dtype, hq=4, hkv=2, dh=64, page=16, lens=[300, 20], slots=304)
+        used = np.isfinite(c["k"])
+        c["k"][used] = C.rounded(c["k"][used] * 1e15, dtype)
+        c["q_scale"] = 1e15
+        q = C.queries(rng, c, 10)
+        scale32 = float(np.float32(scale))
+        dev, x = C.on_gpu(c), C.to_gpu(q, dtype)
+        for window, sinks in ((0, 0), (9, 2)):
+            out, lse = dev.prefill(x, scale=scale, window=window, sinks=sinks, lse=True)
+            ref = O.attend(c, q, [0, 5], [5, 5], scale32, window, sinks)
+            C.check_attention(ref, C.host(out), C.host(lse), dtype, 64)
+            out, lse = dev.decode(x[:2], scale=scale, window=window, sinks=sinks, lse=True)
+            C.check_attention(O.attend(c, q[:2], [0, 1], [1, 1], scale32, window, sinks), C.host(out), C.host(lse), dtype, 64)
