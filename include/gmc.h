@@ -598,6 +598,7 @@ int gmc_cache_append(const gmc_cache* cache, const void* k, const void* v, int64
  *   starts  [n_seq + 1] int32: sequence b's rows of q; at most max_new of them
  *           are computed; NULL: max_new each.  Rows of out that belong to no
  *           sequence are left as they are
+ *   scale   finite
  *   max_new the queries of a sequence's kv head, in blocks of 128, times n_seq
  *           and n_kv_heads must not be more than 2^23 blocks
  *   out     [rows][n_q_heads][head_dim] dtype, 16-byte aligned

@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstdint>
 
 #include "gmc.h"
@@ -69,10 +70,11 @@ int check_new(const char* fn, const CacheView& c, const int32_t* starts, int64_t
   return GMC_OK;
 }
 
-int check_attend(const char* fn, const CacheView& c, const void* q, int64_t q_stride, int64_t window, int64_t sinks,
-                 const void* out) {
+int check_attend(const char* fn, const CacheView& c, const void* q, int64_t q_stride, float scale, int64_t window,
+                 int64_t sinks, const void* out) {
   const int rc = check_rows(fn, "q", c, q, q_stride, static_cast<int64_t>(c.hq) * c.dh);
   if (rc != GMC_OK) return rc;
+  if (!std::isfinite(scale)) return set_error(GMC_ERR_ARG, "%s: scale=%g must be finite", fn, static_cast<double>(scale));
   if (window < 0 || sinks < 0 || window > INT32_MAX || sinks > INT32_MAX)
     return set_error(GMC_ERR_ARG, "%s: window=%lld and sinks=%lld must be in [0, 2^31)", fn, ll(window), ll(sinks));
   if (!out || misaligned(out, 16)) return set_error(GMC_ERR_ARG, "%s: out is NULL or not 16-byte aligned", fn);
@@ -159,7 +161,7 @@ int gmc_cache_decode(const gmc_cache* cache, const void* q, int64_t q_stride, fl
   CacheView c;
   int rc = check_cache(fn, cache, &c);
   if (rc != GMC_OK) return rc;
-  if ((rc = check_attend(fn, c, q, q_stride, window, sinks, out)) != GMC_OK) return rc;
+  if ((rc = check_attend(fn, c, q, q_stride, scale, window, sinks, out)) != GMC_OK) return rc;
   if (accumulate && !c.weights) return set_error(GMC_ERR_ARG, "%s: accumulate needs the cache's weights", fn);
   rc = check_workspace(fn, workspace, workspace_bytes, decode_bytes(c, accumulate != 0));
   if (rc != GMC_OK) return rc;
@@ -185,7 +187,7 @@ int gmc_cache_prefill(const gmc_cache* cache, const void* q, int64_t q_stride, i
   CacheView c;
   int rc = check_cache(fn, cache, &c);
   if (rc != GMC_OK) return rc;
-  if ((rc = check_attend(fn, c, q, q_stride, window, sinks, out)) != GMC_OK) return rc;
+  if ((rc = check_attend(fn, c, q, q_stride, scale, window, sinks, out)) != GMC_OK) return rc;
   if ((rc = check_new(fn, c, starts, max_new, rows)) != GMC_OK) return rc;
   // (a grid has fewer than 2^32 threads, and the kernel counts rows in 32 bits)
   if ((max_new * c.hg + 127) / 128 * c.hkv * c.n_seq > (1ll << 23))

@@ -190,3 +190,11 @@ def test_rows_too_far_apart():
     _refused(B.gmc_cache_append(c, P, P, (1 << 24) + 8, 512, 2, None, None, 1), "2^24")
     _refused(B.gmc_cache_prefill(c, P, (1 << 24) + 8, 2, None, 1, 0.1, 0, 0, P, None, P, 1 << 40), "2^24")
     _refused(B.gmc_cache_decode(c, P, (1 << 24) + 8, 0.1, 0, 0, 0, P, None, P, 1 << 40), "2^24")
+
+
+@pytest.mark.parametrize("scale", [float("nan"), -float("nan"), float("inf"), -float("inf"), 1e39])
+def test_scales_that_are_not_finite(scale):
+    """Both attention calls refuse them alike (1e39 is infinite as a float)."""
+    c = _cache()
+    _refused(B.gmc_cache_prefill(c, P, 3584, 2, None, 1, scale, 0, 0, P, None, P, 1 << 40), "scale")
+    _refused(B.gmc_cache_decode(c, P, 3584, scale, 0, 0, 0, P, None, P, 1 << 40), "scale")
