@@ -9,6 +9,7 @@
 
 #include "gmc.h"
 #include "gmc_cache.h"
+#include "gmc_cache_grid.h"
 #include "gmc_path.h"
 
 namespace {
@@ -189,8 +190,8 @@ int gmc_cache_prefill(const gmc_cache* cache, const void* q, int64_t q_stride, i
   if (rc != GMC_OK) return rc;
   if ((rc = check_attend(fn, c, q, q_stride, scale, window, sinks, out)) != GMC_OK) return rc;
   if ((rc = check_new(fn, c, starts, max_new, rows)) != GMC_OK) return rc;
-  // (a grid has fewer than 2^32 threads, and the kernel counts rows in 32 bits)
-  if ((max_new * c.hg + 127) / 128 * c.hkv * c.n_seq > (1ll << 23))
+  // (what is launched for them is fewer than 2^32 threads, and the kernel counts rows in 32 bits)
+  if ((max_new * c.hg + 127) / 128 * c.hkv * c.n_seq > kPreMaxBlocks)
     return set_error(GMC_ERR_ARG, "%s: more than 2^23 blocks of 128 queries (max_new=%lld, n_seq=%d); split the call",
                      fn, ll(max_new), c.n_seq);
   if ((rc = check_workspace(fn, workspace, workspace_bytes, prefill_bytes(c, max_new))) != GMC_OK) return rc;

@@ -31,6 +31,7 @@
 #include <algorithm>
 
 #include "gmc_cache.h"
+#include "gmc_cache_grid.h"
 #include "gmc_device.h"
 
 namespace gmc {
@@ -110,7 +111,7 @@ struct PreScratch {
   float* part;   // [n_seq * max_new][hq][nsplit][dh] unnormalised sums, or null
   float* ml;     // [n_seq * max_new][hq][nsplit][2] maximum (base 2) and sum
   int nsplit;
-  int run;       // blocks in a row that go to one XCD
+  PreGrid grid;
 };
 // Splits that a block's tiles are shared over: none with fewer than two tiles.
 __device__ __forceinline__ int used_pre_splits(int tiles, int nsplit) { return min(nsplit, max(1, tiles / 2)); }
@@ -126,14 +127,10 @@ prefill_kernel(CacheView c, AttendArgs a, PreScratch sc, int row_blocks) {
   __shared__ __align__(16) unsigned char k_even[KT * PITCH], v_even[KT * PITCH], k_odd[KT * PITCH], v_odd[KT * PITCH];
   __shared__ __align__(16) int pos_even[64], pos_odd[64];   // positions of the tiles' slots, if the window asks for them
 
-  // Each of the eight XCDs (blocks go to them in turn) works on runs of
-  // neighbouring row blocks of a head, whose keys its L2 then holds, and the
-  // runs go round the XCDs, as sequences are of unlike lengths; in a head, rows
-  // with the most keys come first.
-  const int items = row_blocks * sc.nsplit, runs = (items + sc.run - 1) / sc.run;   // of a head
-  const int unit = (blockIdx.x / 8 / sc.run) * 8 + blockIdx.x % 8, bh = unit / runs;
-  const int item = (unit - bh * runs) * sc.run + blockIdx.x / 8 % sc.run;
-  if (bh >= c.hkv * c.n_seq || item >= items) return;
+  // (in a head, rows with the most keys come first)
+  const int heads = c.hkv * c.n_seq;
+  int bh, item;
+  if (!pre_place(sc.grid, blockIdx.x, heads, &bh, &item)) return;
   const int split = item % sc.nsplit, block = row_blocks - 1 - item / sc.nsplit, h = bh % c.hkv, b = bh / c.hkv;
   const PreWork wk = pre_work(c, a, b, block, KT);
   if (wk.rows <= 0) return;
@@ -688,15 +685,10 @@ hipError_t launch_cache_prefill(const CacheView& c, const AttendArgs& a, void* s
     sc.part = static_cast<float*>(scratch);
     sc.ml = sc.part + static_cast<long long>(c.n_seq) * a.max_new * c.hq * sc.nsplit * c.dh;
   }
-  // runs of 32 blocks; shorter ones where that leaves an XCD fewer than eight.
-  // Tokens of one long sequence and ragged short ones, us: 32 944 and 128, 4 958
-  // and 124, 128 1018 and 130.
-  const long long items = static_cast<long long>(row_blocks) * sc.nsplit, heads = static_cast<long long>(c.hkv) * c.n_seq;
-  sc.run = static_cast<int>(std::max<long long>(1, std::min<long long>(32, items * heads / 64)));
-  const long long units = (items + sc.run - 1) / sc.run * heads, total = (units + 7) / 8 * 8 * sc.run;
+  sc.grid = pre_grid(row_blocks * sc.nsplit, static_cast<long long>(c.hkv) * c.n_seq);
 #define GMC_PREFILL(T, DH)                                                                                       \
   case DH:                                                                                                       \
-    hipLaunchKernelGGL((prefill_kernel<T, DH>), dim3(static_cast<unsigned>(total)), dim3(64 * kPreWaves), 0, st, c, a, sc, \
+    hipLaunchKernelGGL((prefill_kernel<T, DH>), dim3(static_cast<unsigned>(sc.grid.blocks)), dim3(64 * kPreWaves), 0, st, c, a, sc, \
                        row_blocks); \
     break;
 #define GMC_PREFILL_ALL(T)                                                                                       \

@@ -856,3 +856,41 @@ def test_scales_far_below_one(scale):
             C.check_attention(ref, C.host(out), C.host(lse), dtype, 64)
             out, lse = dev.decode(x[:2], scale=scale, window=window, sinks=sinks, lse=True)
             C.check_attention(O.attend(c, q[:2], [0, 1], [1, 1], scale32, window, sinks), C.host(out), C.host(lse), dtype, 64)
+
+
+@pytest.mark.parametrize("n_seq,hkv,new", [(65535, 16, 1), (2048, 8, 4), (257, 24, 2)])
+def test_prefill_of_many_short_sequences(n_seq, hkv, new):
+    """More heads than row blocks by far: 2^20 of them, and a few thousand.  The
+    sequences' pages are shared, which reading allows."""
+    _say(f"prefill of {n_seq} sequences, {hkv} heads, {new} tokens")
+    g = torch.Generator("cuda").manual_seed(47)
+    n_pages, page, dh = 40, 16, 32
+    k, v = (torch.randn((n_pages, hkv, page, dh), generator=g, device="cuda").bfloat16() for _ in "kv")
+    table = torch.randint(0, n_pages, (n_seq, 1), generator=g, device="cuda", dtype=torch.int32)
+    lens = torch.randint(0, page + 1, (n_seq,), generator=g, device="cuda", dtype=torch.int32)
+    q = (2 * torch.randn((n_seq * new, hkv, dh), generator=g, device="cuda")).bfloat16()
+    dev = C.B.KvCache(k, v, table, lens, n_q_heads=hkv)
+    out, lse = dev.prefill(q, lse=True)
+    slot, f64 = torch.arange(page, device="cuda"), torch.float64
+    for b0 in range(0, n_seq, 4096):
+        ids, n = table[b0:b0 + 4096, 0].long(), lens[b0:b0 + 4096]
+        rows = slice(b0 * new, (b0 + len(ids)) * new)
+        kk, vv = (x[ids].to(f64) for x in (k, v))                       # [b][h][slot][d]
+        qq = q[rows].view(len(ids), new, hkv, dh).to(f64)
+        ref = {x: [] for x in ("out", "lse", "mass", "size", "most")}
+        for i in range(new):
+            prod = qq[:, i, :, None] * kk                               # [b][h][slot][d]
+            see = (slot <= (n - new + i)[:, None])[:, None].expand(-1, hkv, -1)
+            x = torch.where(see, prod.sum(-1) * dh ** -0.5, -np.inf)
+            m = x.amax(-1, keepdim=True).clamp(min=-1e300)
+            e = torch.exp(x - m)
+            total = e.sum(-1, keepdim=True)
+            a = e / total.clamp(min=1e-300)
+            ref["lse"].append((m + torch.log(total))[..., 0])
+            ref["out"].append((a[..., None] * vv).sum(2))
+            ref["mass"].append((a[..., None] * vv.abs()).sum(2))
+            ref["size"].append(torch.where(see, prod.abs().sum(-1) * dh ** -0.5, 0).amax(-1))
+            ref["most"].append(see.sum(-1).double())
+        ref = {x: torch.stack(y, 1).flatten(0, 1).cpu().numpy() for x, y in ref.items()}
+        ref["lse"][ref["most"] == 0] = -np.inf
+        C.check_attention(ref, C.host(out[rows]), C.host(lse[rows]), "bf16", dh)
