@@ -634,6 +634,7 @@ int gmc_cache_decode(const gmc_cache* cache, const void* q, int64_t q_stride, fl
  * budget.  The slots of such a sequence should be held: a kept row moves only
  * from a page that is one to a page that is one, while its weight and position
  * move all the same.
+ * With more than 8192 slots a sequence, n_seq * n_kv_heads is below 2^22.
  */
 int64_t gmc_cache_evict_bytes(const gmc_cache* cache, int64_t budget);
 int gmc_cache_evict(const gmc_cache* cache, int64_t budget, int64_t sinks, int64_t recent, void* workspace,

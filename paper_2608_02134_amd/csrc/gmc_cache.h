@@ -111,7 +111,9 @@ long long decode_scratch_bytes(const CacheView& c, bool accumulate);
 hipError_t launch_cache_decode(const CacheView& c, const AttendArgs& a, bool accumulate, void* scratch,
                                hipStream_t st);
 
-// scratch: evict_scratch_bytes of any content.
+// scratch: evict_scratch_bytes of any content.  n_seq * hkv: at most
+// evict_max_groups (a launch has fewer than 2^32 threads).
+long long evict_max_groups(const CacheView& c);
 long long evict_scratch_bytes(const CacheView& c);
 hipError_t launch_cache_evict(const CacheView& c, int budget, int sinks, int recent, void* scratch, hipStream_t st);
 

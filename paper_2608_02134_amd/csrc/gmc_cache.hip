@@ -219,6 +219,9 @@ int gmc_cache_evict(const gmc_cache* cache, int64_t budget, int64_t sinks, int64
     return set_error(GMC_ERR_ARG, "%s: need budget >= 1 and sinks + recent <= budget, none negative (budget=%lld "
                      "sinks=%lld recent=%lld)", fn, ll(budget), ll(sinks), ll(recent));
   if (budget >= c.cap) return GMC_OK;   // no sequence can hold more
+  if (ll(c.n_seq) * c.hkv > evict_max_groups(c))
+    return set_error(GMC_ERR_ARG, "%s: more than %lld caches of a head (n_seq=%d, n_kv_heads=%d); split the call", fn,
+                     evict_max_groups(c), c.n_seq, c.hkv);
   rc = check_workspace(fn, workspace, workspace_bytes, evict_bytes(c));
   if (rc != GMC_OK) return rc;
   return on_stream(fn, stream, [&](hipStream_t st) {

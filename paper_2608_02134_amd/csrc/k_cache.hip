@@ -105,6 +105,8 @@ hipError_t launch_cache_append(const CacheView& c, const void* k, const void* v,
     hipLaunchKernelGGL(cache_append_few_kernel, dim3(c.n_seq), dim3(256), 0, st, c, a);
   } else {
     hipLaunchKernelGGL(cache_append_kernel, dim3(std::min((max_new + 3) / 4, 4096), c.n_seq), dim3(256), 0, st, c, a);
+    const hipError_t err = hipGetLastError();
+    if (err != hipSuccess) return err;   // (rows that were not written are not counted)
     hipLaunchKernelGGL(cache_advance_kernel, dim3((c.n_seq + 255) / 256), dim3(256), 0, st, c, a);
   }
   return hipGetLastError();
@@ -145,6 +147,7 @@ __device__ __forceinline__ uint32_t evict_key(float w, bool safe) {
 constexpr int kEvictBins = 2048, kEvictList = 256, kEvictRuns = 16, kEvictHead = 64;
 constexpr int kEvictShort = 8192;                  // slots of a cache whose halves shared memory holds
 constexpr int kEvictSlice = 4096;                  // slots a block of the first kernel takes
+constexpr int kEvictThreads = 1024;                // threads of the selecting block of a long cache
 constexpr uint32_t kSafeHalf = 0xFFFFu;            // protected; others are at most 0xFF81
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 
@@ -593,6 +596,10 @@ evict_move_kernel(CacheView c, int budget, EvictLists in, int chunks) {
   if (h == 0 && blockIdx.y == 0 && threadIdx.x == 0) c.lens[b] = min(cache_len(c, b), budget);
 }
 
+long long evict_max_groups(const CacheView& c) {
+  return ((1ll << 32) - 1) / (c.cap <= kEvictShort ? 256 : kEvictThreads);
+}
+
 long long evict_scratch_bytes(const CacheView& c) {
   const long long groups = static_cast<long long>(c.n_seq) * c.hkv;
   const long long lists = 4 * groups * (kEvictHead + 2ll * c.cap);
@@ -614,8 +621,12 @@ hipError_t launch_cache_evict(const CacheView& c, int budget, int sinks, int rec
   } else {
     hipLaunchKernelGGL(evict_halves_kernel, dim3(groups, evict_slices(c.cap)), dim3(256), 0, st, c, budget, sinks, recent,
                        lists);
-    hipLaunchKernelGGL((evict_select_kernel<1024, 0>), dim3(groups), dim3(1024), 0, st, c, budget, sinks, recent, lists);
+    const hipError_t err = hipGetLastError();
+    if (err != hipSuccess) return err;
+    hipLaunchKernelGGL((evict_select_kernel<kEvictThreads, 0>), dim3(groups), dim3(kEvictThreads), 0, st, c, budget, sinks, recent, lists);
   }
+  const hipError_t err = hipGetLastError();
+  if (err != hipSuccess) return err;   // (the lists that the next kernel follows were not written)
   const long long total = static_cast<long long>(std::min(c.cap - budget, budget)) * chunks;   // pieces that can move
   const int gy =
       static_cast<int>(std::max<long long>(1, std::min<long long>((total + 256 * kMoveDepth - 1) / (256 * kMoveDepth), 1024)));

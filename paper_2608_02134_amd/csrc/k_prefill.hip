@@ -700,6 +700,8 @@ hipError_t launch_cache_prefill(const CacheView& c, const AttendArgs& a, void* s
   if (c.dtype == 0) { GMC_PREFILL_ALL(float) } else { GMC_PREFILL_ALL(bf16_t) }
 #undef GMC_PREFILL_ALL
 #undef GMC_PREFILL
+  const hipError_t err = hipGetLastError();
+  if (err != hipSuccess) return err;   // (there is nothing to join)
   if (sc.nsplit > 1) {
     const dim3 grid((a.max_new + 3) / 4, c.hq, c.n_seq);
     if (c.dtype == 0)

@@ -198,3 +198,14 @@ def test_scales_that_are_not_finite(scale):
     c = _cache()
     _refused(B.gmc_cache_prefill(c, P, 3584, 2, None, 1, scale, 0, 0, P, None, P, 1 << 40), "scale")
     _refused(B.gmc_cache_decode(c, P, 3584, scale, 0, 0, 0, P, None, P, 1 << 40), "scale")
+
+
+def test_eviction_of_more_caches_than_a_launch_takes():
+    """Long caches take 1024 threads a head, short ones 256; a launch has fewer than
+    2^32.  (What passes is not run: it would need a device.)"""
+    many = dict(n_q_heads=256, n_kv_heads=256, head_dim=32)
+    _refused(B.gmc_cache_evict(_cache(n_seq=16384, max_pages=513, **many), 50, 4, 4, P, 1 << 62), "4194303 caches")
+    _refused(B.gmc_cache_evict(_cache(n_seq=65535, max_pages=1 << 20, **many), 50, 4, 4, P, 1 << 62), "4194303 caches")
+    if not torch.cuda.is_available():
+        assert B.gmc_cache_evict(_cache(n_seq=16383, max_pages=513, **many), 50, 4, 4, P, 1 << 62) == B.GMC_ERR_HIP
+        assert B.gmc_cache_evict(_cache(n_seq=65535, max_pages=512, **many), 50, 4, 4, P, 1 << 62) == B.GMC_ERR_HIP
