@@ -643,6 +643,8 @@ def check_cache_tensors(k_pages, v_pages, page_table, lens, n_q_heads, slot_pos=
         raise ValueError("v_pages must have k_pages' shape and dtype")
     if page_table.dim() != 2 or page_table.dtype != torch.int32:
         raise ValueError("page_table must be int32 [n_seq][max_pages]")
+    if k_pages.numel() == 0 or page_table.numel() == 0:
+        raise ValueError(f"k_pages {tuple(k_pages.shape)} and page_table {tuple(page_table.shape)} must not be empty")
     b, slots = page_table.shape[0], page_table.shape[1] * k_pages.shape[2]
     if n_q_heads < 1 or n_q_heads % max(k_pages.shape[1], 1) != 0:
         raise ValueError(f"n_q_heads={n_q_heads} must be a multiple of the cache's {k_pages.shape[1]} kv heads")
@@ -709,6 +711,8 @@ class KvCache:
         """An empty cache of `slots` slots a sequence (rounded up to whole
         pages), its pages in order; ``evicts`` adds positions and weights."""
         import torch
+        if n_seq < 1 or slots < 1 or page_size < 1:
+            raise ValueError(f"n_seq={n_seq}, slots={slots} and page_size={page_size} must be at least 1")
         per = -(-slots // page_size)
         pages = [torch.zeros((n_seq * per, n_kv_heads, page_size, head_dim), dtype=dtype, device=device) for _ in "kv"]
         table = torch.arange(n_seq * per, dtype=torch.int32, device=device).view(n_seq, per)

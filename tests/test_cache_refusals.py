@@ -209,3 +209,21 @@ def test_eviction_of_more_caches_than_a_launch_takes():
     if not torch.cuda.is_available():
         assert B.gmc_cache_evict(_cache(n_seq=16383, max_pages=513, **many), 50, 4, 4, P, 1 << 62) == B.GMC_ERR_HIP
         assert B.gmc_cache_evict(_cache(n_seq=65535, max_pages=512, **many), 50, 4, 4, P, 1 << 62) == B.GMC_ERR_HIP
+
+
+@pytest.mark.parametrize("over", [
+    dict(page_table=torch.zeros((0, 3), dtype=torch.int32), lens=torch.zeros(0, dtype=torch.int32), slot_pos=None, weights=None,
+         seen=None),
+    dict(page_table=torch.zeros((2, 0), dtype=torch.int32), slot_pos=None, weights=None),
+    dict(k_pages=torch.zeros((6, 0, 16, 64)), v_pages=torch.zeros((6, 0, 16, 64)), slot_pos=None, weights=None),
+    dict(k_pages=torch.zeros((0, 2, 16, 64)), v_pages=torch.zeros((0, 2, 16, 64)))])
+def test_wrapper_rejects_empty_caches(over):
+    with pytest.raises(ValueError, match="must not be empty"):
+        B.check_cache_tensors(**_tensors(**over))
+
+
+@pytest.mark.parametrize("over", [dict(n_seq=0), dict(slots=0), dict(page_size=0), dict(slots=-5)])
+def test_wrapper_creates_no_empty_caches(over):
+    args = dict(n_seq=2, slots=40, n_q_heads=4, n_kv_heads=2, head_dim=64, dtype=torch.bfloat16, device="cpu")
+    with pytest.raises(ValueError, match="at least 1"):
+        B.KvCache.create(**{**args, **over})
