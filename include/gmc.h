@@ -519,6 +519,11 @@ int gmc_prune_static(const gmc_config* cfg, int64_t B, const void* hidden, const
  *   page_table [n_seq][max_pages] int32.  Entries past a sequence's length are
  *              not used; a slot on an id outside [0, n_pages) counts as not
  *              held: attention does not see it, appending leaves it out
+ *              Sequences may share pages that are only read (the whole pages of
+ *              a common prefix).  A page that a call writes must stand once in
+ *              the table: appending writes the slots behind a sequence's last,
+ *              and eviction moves rows within all pages of a sequence that it
+ *              cuts, so sequences with shared pages are not evicted from
  *   lens       [n_seq] int32, slots held; read as clamped to [0, max_pages *
  *              page_size].  Slots at and past the length are never read as
  *              rows, whatever they hold

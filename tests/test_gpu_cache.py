@@ -894,3 +894,24 @@ def test_prefill_of_many_short_sequences(n_seq, hkv, new):
         ref = {x: torch.stack(y, 1).flatten(0, 1).cpu().numpy() for x, y in ref.items()}
         ref["lse"][ref["most"] == 0] = -np.inf
         C.check_attention(ref, C.host(out[rows]), C.host(lse[rows]), "bf16", dh)
+
+
+def test_sequences_that_share_the_pages_of_a_common_prefix():
+    """Two whole pages and a half belong to a prompt that three sequences begin
+    with: the whole ones are shared, what is appended to is each one's own."""
+    _say("shared prefix")
+    rng = np.random.default_rng(45)
+    c = C.make(rng, dtype="bf16", hq=8, hkv=2, dh=64, page=16, lens=[32, 32, 32], slots=80)
+    c["table"][1, :2] = c["table"][2, :2] = c["table"][0, :2]
+    q, m = C.queries(rng, c, 3 * 21), 21
+    kv = C.rounded(rng.standard_normal((3 * m, 2, 2, 64)), "bf16")
+    dev, x = C.on_gpu(c), C.to_gpu(kv, "bf16")
+    shared = dev.k_pages[dev.page_table[0, :2].long()].clone()
+    dev.append(x[:, 0], x[:, 1])
+    O.append(c, kv[:, 0], kv[:, 1], [m] * 3, [np.arange(i * m, (i + 1) * m) for i in range(3)])
+    _compare_caches(c, dev)
+    assert torch.equal(shared, dev.k_pages[dev.page_table[0, :2].long()])
+    out, lse = dev.prefill(C.to_gpu(q, "bf16"), lse=True)
+    C.check_attention(O.attend(c, q, [0, m, 2 * m], [m] * 3, 0.125), C.host(out), C.host(lse), "bf16", 64)
+    out, lse = dev.decode(C.to_gpu(q[:3], "bf16"), lse=True)
+    C.check_attention(O.attend(c, q[:3], [0, 1, 2], [1] * 3, 0.125), C.host(out), C.host(lse), "bf16", 64)
