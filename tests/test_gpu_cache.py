@@ -915,3 +915,47 @@ def test_sequences_that_share_the_pages_of_a_common_prefix():
     C.check_attention(O.attend(c, q, [0, m, 2 * m], [m] * 3, 0.125), C.host(out), C.host(lse), "bf16", 64)
     out, lse = dev.decode(C.to_gpu(q[:3], "bf16"), lse=True)
     C.check_attention(O.attend(c, q[:3], [0, 1, 2], [1] * 3, 0.125), C.host(out), C.host(lse), "bf16", 64)
+
+
+def test_captured_steps_replay_the_whole_state():
+    """Append, windowed decode with accumulation and eviction in one graph: after
+    each replay every weight, position and row of the live slots and all pages are
+    those of the same calls made eagerly."""
+    _say("graph, whole state")
+    rng = np.random.default_rng(43)
+    args = dict(dtype="bf16", hq=14, hkv=2, dh=128, page=16, lens=[300, 60], slots=320, positions=True, weights=True)
+    a, b = C.on_gpu(C.make(np.random.default_rng(44), **args)), C.on_gpu(C.make(np.random.default_rng(44), **args))
+    kv = torch.zeros((2, 2, 2, 128), dtype=torch.bfloat16, device="cuda")
+    q = torch.zeros((2, 14, 128), dtype=torch.bfloat16, device="cuda")
+
+    def step(cache):
+        cache.append(kv[:, 0], kv[:, 1])
+        out, lse = cache.decode(q, window=150, sinks=2, accumulate=True, lse=True)
+        cache.evict(200, sinks=2, recent=9)
+        return out, lse
+
+    state = lambda x: (x.lens, x.seen, x.slot_pos, x.weights, x.k_pages, x.v_pages)  # noqa: E731
+    keep = [t.clone() for t in state(a)]
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step(a)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(a)
+    for t, s in zip(state(a), keep):
+        t.copy_(s)
+    for i in range(5):
+        kv.copy_(torch.from_numpy(rng.standard_normal(kv.shape)).cuda())
+        q.copy_(torch.from_numpy(rng.standard_normal(q.shape)).cuda())
+        graph.replay()
+        want = step(b)
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), i
+        assert torch.equal(a.lens, b.lens) and torch.equal(a.seen, b.seen), i
+        assert a.lens.tolist() == [200, 61 + i]
+        for seq, n in enumerate(a.lens.tolist()):
+            assert torch.equal(a.weights[seq, :, :n], b.weights[seq, :, :n]), (i, seq)
+            assert torch.equal(a.slot_pos[seq, :, :n], b.slot_pos[seq, :, :n]), (i, seq)
+        for x, y in ((a.k_pages, b.k_pages), (a.v_pages, b.v_pages)):
+            assert torch.equal(_bits(x), _bits(y)), i     # (slots that hold nothing are NaN in both)
