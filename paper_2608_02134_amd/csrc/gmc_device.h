@@ -16,7 +16,9 @@ __device__ __forceinline__ float bf16_to_f32(bf16_t v) {
   return __uint_as_float(static_cast<uint32_t>(v) << 16);
 }
 
-// Round-to-nearest-even float -> bf16 (finite inputs).
+// Round-to-nearest-even float -> bf16.  Finite inputs and infinities; of NaN those
+// whose lower 16 bits are zero, as are all that come of bf16 values or of an
+// invalid operation (others may round to an infinity or zero).
 __device__ __forceinline__ bf16_t f32_to_bf16(float f) {
   uint32_t u = __float_as_uint(f);
   u += 0x7FFFu + ((u >> 16) & 1u);

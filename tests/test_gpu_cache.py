@@ -959,3 +959,31 @@ def test_captured_steps_replay_the_whole_state():
             assert torch.equal(a.slot_pos[seq, :, :n], b.slot_pos[seq, :, :n]), (i, seq)
         for x, y in ((a.k_pages, b.k_pages), (a.v_pages, b.v_pages)):
             assert torch.equal(_bits(x), _bits(y)), i     # (slots that hold nothing are NaN in both)
+
+
+@pytest.mark.parametrize("bits", [0x7FFF, -1, 0x7F81, -127, 0x7FC0, -64])
+@pytest.mark.parametrize("where", ["q", "k", "v"])
+def test_a_nan_of_any_payload_stays_one(bits, where):
+    """bf16 NaN with all, one and the usual mantissa bits, of either sign, quiet or
+    not: the outputs that it reaches are NaN, in one block and joined from splits."""
+    _say(f"NaN {bits & 0xFFFF:#x} in {where}")
+    nan = torch.tensor(bits, dtype=torch.int16, device="cuda").view(torch.bfloat16)
+    assert torch.isnan(nan)
+    for slots in (64, 3008):
+        rng = np.random.default_rng(48)
+        c = C.make(rng, dtype="bf16", hq=4, hkv=2, dh=64, page=16, lens=[slots, slots - 7], slots=slots)
+        q = C.to_gpu(C.queries(rng, c, 2), "bf16")
+        dev = C.on_gpu(c)
+        if where == "q":
+            q[0, 1] = nan
+            hit = [(0, 1)]
+        else:
+            p, r = O.row_of(c, 0, 0, slots // 2)
+            {"k": dev.k_pages, "v": dev.v_pages}[where][p, 0, r] = nan
+            hit = [(0, 0), (0, 1)]
+        for out, lse in (dev.prefill(q, lse=True), dev.decode(q, lse=True)):
+            for b in range(2):
+                for h in range(4):
+                    bad = torch.isnan(out[b, h])
+                    assert bad.all() if (b, h) in hit else not bad.any(), (slots, b, h)
+                    assert torch.isnan(lse[b, h]).item() == ((b, h) in hit and where != "v"), (slots, b, h)
