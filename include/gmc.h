@@ -518,7 +518,7 @@ int gmc_prune_static(const gmc_config* cfg, int64_t B, const void* hidden, const
  *              aligned; the keys as attention uses them (post-norm, post-rotary)
  *   page_table [n_seq][max_pages] int32.  Entries past a sequence's length are
  *              not used; a slot on an id outside [0, n_pages) counts as not
- *              held: attention does not see it, appending leaves it out
+ *              held: attention does not see it, appending leaves it out.
  *              Sequences may share pages that are only read (the whole pages of
  *              a common prefix).  A page that a call writes must stand once in
  *              the table: appending writes the slots behind a sequence's last,

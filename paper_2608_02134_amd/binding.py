@@ -788,8 +788,10 @@ class KvCache:
         if src is not None:
             if starts is not None:
                 raise ValueError("src and starts must not both be given")
-            max_new = src.shape[1] if src.dim() == 2 else 0
-            first, taken = None, self._index("src", src, (self.n_seq, max_new))
+            n = src.shape[1] if src.dim() == 2 else 0
+            if max_new is not None and max_new != n:
+                raise ValueError(f"max_new={max_new} must be the {n} columns of src, or not be given")
+            first, max_new, taken = None, n, self._index("src", src, (self.n_seq, n))
         else:
             (first, max_new), taken = self._new(rows, starts, max_new), None
         self._call("gmc_cache_append", k.data_ptr(), v.data_ptr(), sk, sv, rows, first, taken, max_new)

@@ -987,3 +987,18 @@ def test_a_nan_of_any_payload_stays_one(bits, where):
                     bad = torch.isnan(out[b, h])
                     assert bad.all() if (b, h) in hit else not bad.any(), (slots, b, h)
                     assert torch.isnan(lse[b, h]).item() == ((b, h) in hit and where != "v"), (slots, b, h)
+
+
+def test_max_new_beside_src():
+    """It was taken for the columns of src whatever it said."""
+    _say("max_new beside src")
+    c = C.make(np.random.default_rng(49), dtype="bf16", hq=4, hkv=2, dh=64, page=16, lens=[30, 40], slots=64)
+    dev = C.on_gpu(c)
+    k = torch.zeros((4, 2, 64), dtype=torch.bfloat16, device="cuda")
+    src = torch.zeros((2, 2), dtype=torch.int32, device="cuda")
+    for n in (0, 1, 3):
+        with pytest.raises(ValueError, match="max_new"):
+            dev.append(k, k, src=src, max_new=n)
+    assert dev.lens.tolist() == [30, 40]
+    dev.append(k, k, src=src, max_new=2)
+    assert dev.lens.tolist() == [32, 42]
