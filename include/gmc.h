@@ -580,7 +580,9 @@ typedef struct gmc_cache {
  *           rows - the keep list of gmc_compact_sequence puts a prefix
  *           layer's retained K/V into the cache without a gathered copy.
  *           Indices are clamped
- * Rows past the capacity are left out, and lens and seen stop there.
+ * rows and max_new are at least 1.  Rows past the capacity are left out, and
+ * lens and seen stop there: the last slots are then not those of the last
+ * tokens, so a caller that attends from the new tokens leaves room for all.
  */
 int gmc_cache_append(const gmc_cache* cache, const void* k, const void* v, int64_t k_stride, int64_t v_stride,
                      int64_t rows, const int32_t* starts, const int32_t* src, int64_t max_new, void* stream);
@@ -631,7 +633,8 @@ int gmc_cache_decode(const gmc_cache* cache, const void* q, int64_t q_stride, fl
  * gmc_cache_evict - every sequence that holds more than `budget` slots keeps
  * `budget` of them, chosen per kv head: first the rows whose position is
  * below `sinks` or among the last `recent` positions seen, then those of
- * largest accumulated weight (ties to the lower slot; NaN counts as lowest).
+ * largest accumulated weight (ties to the lower slot; NaN counts as lowest;
+ * appended rows weigh 0 until gmc_cache_decode adds to them).
  * Attention does not depend on the order of the slots, so only the slots
  * below the budget whose rows leave are filled: the i-th of them takes the
  * i-th kept slot at or above the budget - K, V, position and weight.  lens
