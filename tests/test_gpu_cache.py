@@ -1002,3 +1002,34 @@ def test_max_new_beside_src():
     assert dev.lens.tolist() == [30, 40]
     dev.append(k, k, src=src, max_new=2)
     assert dev.lens.tolist() == [32, 42]
+
+
+@pytest.mark.parametrize("seed", range(16))
+def test_infinities_and_nan_where_the_formula_has_them(seed):
+    """Random layouts with a few value rows of infinities and NaN: each output is
+    the infinity or NaN of the formula or within the bounds, in prefill and decode."""
+    rng = np.random.default_rng(1000 + seed)
+    dtype, dh, page = ("bf16", "f32")[seed % 2], 32 * (seed // 2 + 1), int(2 ** rng.integers(4, 8))
+    hkv, b, slots = int(rng.integers(1, 4)), int(rng.integers(1, 4)), int(rng.integers(40, 500))
+    hq, lens = hkv * int(rng.integers(1, 9)), [int(n) for n in rng.integers(1, slots + 1, b)]
+    window, sinks = (0, 0) if rng.random() < 0.3 else (int(rng.integers(1, slots)), int(rng.integers(0, 9)))
+    c = C.make(rng, dtype=dtype, hq=hq, hkv=hkv, dh=dh, page=page, lens=lens, slots=slots, positions=bool(rng.integers(2)),
+               q_scale=1.0)
+    _say(f"infinities {dtype} {hq} on {hkv} of {dh}, {lens}, window {window}")
+    for bad in (np.nan, np.inf, -np.inf, np.inf):
+        seq, d = int(rng.integers(b)), int(rng.integers(dh))
+        p, r = O.row_of(c, seq, 0, int(rng.integers(lens[seq])))
+        c["v"][p, int(rng.integers(hkv)), r, d:d + 20] = bad
+    new = [min(n, 50) for n in lens]
+    first = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    q, dev = C.queries(rng, c, int(first[-1])), C.on_gpu(c)
+    x = C.to_gpu(q, dtype)
+    calls = [(dev.prefill(x, starts=torch.from_numpy(first).cuda(), max_new=max(new), window=window, sinks=sinks, lse=True),
+              O.attend(c, q, first[:-1], new, dh ** -0.5, window, sinks)),
+             (dev.decode(x[:b], window=window, sinks=sinks, lse=True),
+              O.attend(c, q[:b], list(range(b)), [1] * b, dh ** -0.5, window, sinks))]
+    for (out, lse), ref in calls:
+        out, odd = C.host(out), ~np.isfinite(ref["out"])
+        assert np.array_equal(out[odd], ref["out"][odd], equal_nan=True)
+        ref["out"][odd] = ref["mass"][odd] = out[odd] = 0
+        C.check_attention(ref, out, C.host(lse), dtype, dh)

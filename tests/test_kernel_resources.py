@@ -111,3 +111,12 @@ def test_selections_side_by_side_never_wait_for_each_others_room(built, limits):
                     assert not _stuck(rng, (a, limits["kHalfLds"]), (b, lds_b), limits["kGateRegs"]), (a, b, lds_b)
     whole = max(r for _, r, _, h in _variants(built) if not h)
     assert any(_stuck(rng, (whole, limits["kHalfLds"]), (half[-1], limits["kHalfLds"]), 0) for _ in range(3))
+
+
+def test_cache_attention_keeps_its_registers(built):
+    """No head dimension (32..256) of the cache's attention spills to scratch, in
+    either type, but prefill's widest fp32 one by a few values."""
+    found = _find(built, r"(prefill|decode_split)_kernel")
+    assert len(found) == 16 + 16 + 8
+    spilt = {n: k[".private_segment_fixed_size"] for n, k in found.items() if k[".private_segment_fixed_size"]}
+    assert all("prefill_kernelIfLi256" in n and size <= 64 for n, size in spilt.items()), spilt
