@@ -679,6 +679,8 @@ class KvCache:
     that evicts also ``seen`` [n_seq] int32, ``slot_pos``
     [n_seq][n_kv_heads][slots] int32 and ``weights`` of the same shape, float32.
     The calls work on these very tensors: change them in place.
+    Sequences may share pages that are only read, not those that are appended to
+    or evicted from.
     """
 
     def __init__(self, k_pages, v_pages, page_table, lens, *, n_q_heads, slot_pos=None, seen=None, weights=None):

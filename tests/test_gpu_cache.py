@@ -897,8 +897,8 @@ def test_prefill_of_many_short_sequences(n_seq, hkv, new):
 
 
 def test_sequences_that_share_the_pages_of_a_common_prefix():
-    """Two whole pages and a half belong to a prompt that three sequences begin
-    with: the whole ones are shared, what is appended to is each one's own."""
+    """Three sequences begin with the same two whole pages; what is appended to is
+    each one's own."""
     _say("shared prefix")
     rng = np.random.default_rng(45)
     c = C.make(rng, dtype="bf16", hq=8, hkv=2, dh=64, page=16, lens=[32, 32, 32], slots=80)
