@@ -648,6 +648,127 @@ int64_t gmc_cache_evict_bytes(const gmc_cache* cache, int64_t budget);
 int gmc_cache_evict(const gmc_cache* cache, int64_t budget, int64_t sinks, int64_t recent, void* workspace,
                     int64_t workspace_bytes, void* stream);
 
+/*
+ * gmc_rotary - a host struct that describes a rotary position encoding by its
+ * table; read during the call only.  Pair j of a head's first rot_dim elements
+ * turns by the angle whose cosine and sine stand in column j of the row of the
+ * token's position:
+ *   (x, y) -> (x cos - y sin, y cos + x sin)
+ * in fp32 without fused products, rounded once to the dtype.  Elements from
+ * rot_dim on stay as they are.
+ *   cos, sin   [n_pos][rot_dim / 2] float32, device memory of the caller, 16-byte
+ *              aligned.  Any frequencies and scalings are the table's
+ *   rot_dim    a positive multiple of 16, at most head_dim
+ *   interleaved 0: pair j is elements (j, j + rot_dim / 2); 1: (2 j, 2 j + 1)
+ *   sections   all 0: one position a token.  Otherwise three numbers t, h, w a
+ *              token, of which the first sections[0] pairs take t, the next
+ *              sections[1] h and the last sections[2] w: multiples of 4 (0 is
+ *              fine), rot_dim / 2 together
+ * Positions are clamped to [0, n_pos).
+ */
+typedef struct gmc_rotary {
+  const float* cos;
+  const float* sin;
+  int64_t n_pos;         /* at least 1, below 2^31 */
+  int32_t rot_dim;
+  int32_t interleaved;
+  int32_t sections[3];
+} gmc_rotary;
+
+/*
+ * gmc_cache_append_rotary - gmc_cache_append with the position rotation on the
+ * way: keys that are not rotated yet are stored as attention uses them, the
+ * tokens' queries are rotated by the same call.  k, v, strides, rows, starts,
+ * src and max_new as there; every slot, position, weight and length is left as
+ * gmc_cache_append leaves it.
+ *   pos     [rows] int32, or [rows][3] with sections: the position of each row
+ *           of k (with src: of each row that is picked from, as
+ *           gmc_compact_sequence leaves a sequence's).  NULL: the position that
+ *           the slot gets, seen[b] + i, or lens[b] + i in a cache without seen,
+ *           for all of t, h and w
+ *   q       rows of n_q_heads * head_dim elements, q_stride elements apart, one
+ *           for each row of k; NULL: no queries (q_out is NULL too)
+ *   q_out   [n][n_q_heads][head_dim] dtype, 16-byte aligned: the rotated query of
+ *           every new token, n = rows, in the row of its q; with src n = n_seq *
+ *           max_new, sequence after sequence.  Rows of no sequence are left as
+ *           they are; tokens past the capacity have theirs all the same.
+ *           Without src it may be q itself, if q_stride is n_q_heads * head_dim;
+ *           it must not overlap anything else that the call reads
+ * Errors as of the cache's calls.
+ */
+int gmc_cache_append_rotary(const gmc_cache* cache, const gmc_rotary* rotary, const void* k, const void* v,
+                            int64_t k_stride, int64_t v_stride, int64_t rows, const int32_t* starts,
+                            const int32_t* src, int64_t max_new, const int32_t* pos, const void* q, int64_t q_stride,
+                            void* q_out, void* stream);
+
+/*
+ * gmc_cache4 - a paged K/V cache held in 4 bits (4.25 with the scales), as
+ * gmc_cache otherwise: page_table, lens, sharing of pages, clamping, streams,
+ * scratch memory and errors are the same.  Slots are in order (a slot's
+ * position is its index): there is no eviction from it.
+ * Every 32 neighbouring elements of a row of a head are a block with one scale,
+ * a byte e for 2^(e - 127) (255: the block reads as NaN), and 32 codes of 4 bits:
+ * bit 3 is the sign, bits 2..0 number the magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6.
+ * Byte i of a row's codes holds element 2 i in its lower half and 2 i + 1 in its
+ * upper one.  A value is code times scale; each is a bfloat16 exactly.
+ *   k_codes, v_codes   [n_pages][n_kv_heads][page_size][head_dim / 2] bytes,
+ *                      16-byte aligned
+ *   k_scales, v_scales [n_pages][n_kv_heads][page_size][S] bytes, 16-byte
+ *                      aligned; S is head_dim / 32 rounded up to a power of two,
+ *                      the bytes from head_dim / 32 on are not used
+ * dtype is that of k, v, q and out.
+ */
+typedef struct gmc_cache4 {
+  int32_t dtype;
+  int32_t n_q_heads, n_kv_heads, head_dim;
+  int32_t page_size;
+  int32_t max_pages;
+  int64_t n_pages;
+  int64_t n_seq;
+  void* k_codes;
+  void* v_codes;
+  void* k_scales;
+  void* v_scales;
+  const int32_t* page_table;
+  int32_t* lens;
+} gmc_cache4;
+
+/*
+ * gmc_cache4_append - gmc_cache_append, or gmc_cache_append_rotary with `rotary`
+ * not NULL, into a cache of 4 bits.  A block's scale is the least power of two
+ * from 2^-126 on for which no magnitude of the (rotated, fp32) block is above 7
+ * scales, and each element becomes the nearest code, ties to the even one: off by
+ * at most a quarter of the scale up to 2 scales, half up to 4, one above.  A block
+ * with an infinity or NaN gets scale 255.  Without rotary, pos, q and q_out must
+ * be NULL.
+ */
+int gmc_cache4_append(const gmc_cache4* cache, const gmc_rotary* rotary, const void* k, const void* v,
+                      int64_t k_stride, int64_t v_stride, int64_t rows, const int32_t* starts, const int32_t* src,
+                      int64_t max_new, const int32_t* pos, const void* q, int64_t q_stride, void* q_out,
+                      void* stream);
+
+/*
+ * gmc_cache4_read - the values of the n_b newest slots of each sequence: row
+ * first_b + i of k_out and v_out ([rows][n_kv_heads][head_dim] dtype, 16-byte
+ * aligned) receives slot lens[b] - n_b + i, zeros where that is no slot or its
+ * page is none.  rows, starts and max_new as for gmc_cache_prefill; rows of no
+ * sequence are left as they are.
+ */
+int gmc_cache4_read(const gmc_cache4* cache, int64_t rows, const int32_t* starts, int64_t max_new, void* k_out,
+                    void* v_out, void* stream);
+
+/*
+ * gmc_cache4_prefill, gmc_cache4_decode - gmc_cache_prefill and gmc_cache_decode
+ * (without accumulated weights) over the values of a cache of 4 bits.
+ */
+int64_t gmc_cache4_prefill_bytes(const gmc_cache4* cache, int64_t max_new);
+int gmc_cache4_prefill(const gmc_cache4* cache, const void* q, int64_t q_stride, int64_t rows, const int32_t* starts,
+                       int64_t max_new, float scale, int64_t window, int64_t sinks, void* out, float* lse,
+                       void* workspace, int64_t workspace_bytes, void* stream);
+int64_t gmc_cache4_decode_bytes(const gmc_cache4* cache);
+int gmc_cache4_decode(const gmc_cache4* cache, const void* q, int64_t q_stride, float scale, int64_t window,
+                      int64_t sinks, void* out, float* lse, void* workspace, int64_t workspace_bytes, void* stream);
+
 /* Bytes of device workspace the current context holds (0 without one). */
 int64_t gmc_workspace_bytes(void);
 

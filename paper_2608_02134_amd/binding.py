@@ -95,6 +95,20 @@ class GmcCache(ctypes.Structure):
                 ("slot_pos", _vp), ("weights", _vp)]
 
 
+class GmcRotary(ctypes.Structure):
+    """Mirror of ``gmc_rotary``: the table of a rotary position encoding."""
+    _fields_ = [("cos", _vp), ("sin", _vp), ("n_pos", _i64), ("rot_dim", _i32), ("interleaved", _i32),
+                ("sections", _i32 * 3)]
+
+
+class GmcCache4(ctypes.Structure):
+    """Mirror of ``gmc_cache4``: one layer's paged K/V cache in 4 bits."""
+    _fields_ = [("dtype", _i32), ("n_q_heads", _i32), ("n_kv_heads", _i32), ("head_dim", _i32),
+                ("page_size", _i32), ("max_pages", _i32), ("n_pages", _i64), ("n_seq", _i64),
+                ("k_codes", _vp), ("v_codes", _vp), ("k_scales", _vp), ("v_scales", _vp), ("page_table", _vp),
+                ("lens", _vp)]
+
+
 # name -> (restype, argtypes) of every symbol include/gmc.h declares
 SIGNATURES = {
     "gmc_config_default": (None, [ctypes.POINTER(GmcConfig)]),
@@ -132,6 +146,17 @@ SIGNATURES = {
                                         _i64, _vp]),
     "gmc_cache_evict_bytes": (_i64, [ctypes.POINTER(GmcCache), _i64]),
     "gmc_cache_evict": (ctypes.c_int, [ctypes.POINTER(GmcCache), _i64, _i64, _i64, _vp, _i64, _vp]),
+    "gmc_cache_append_rotary": (ctypes.c_int, [ctypes.POINTER(GmcCache), ctypes.POINTER(GmcRotary), _vp, _vp, _i64,
+                                               _i64, _i64, _vp, _vp, _i64, _vp, _vp, _i64, _vp, _vp]),
+    "gmc_cache4_append": (ctypes.c_int, [ctypes.POINTER(GmcCache4), ctypes.POINTER(GmcRotary), _vp, _vp, _i64, _i64,
+                                         _i64, _vp, _vp, _i64, _vp, _vp, _i64, _vp, _vp]),
+    "gmc_cache4_read": (ctypes.c_int, [ctypes.POINTER(GmcCache4), _i64, _vp, _i64, _vp, _vp, _vp]),
+    "gmc_cache4_prefill_bytes": (_i64, [ctypes.POINTER(GmcCache4), _i64]),
+    "gmc_cache4_prefill": (ctypes.c_int, [ctypes.POINTER(GmcCache4), _vp, _i64, _i64, _vp, _i64, _f32, _i64, _i64,
+                                          _vp, _vp, _vp, _i64, _vp]),
+    "gmc_cache4_decode_bytes": (_i64, [ctypes.POINTER(GmcCache4)]),
+    "gmc_cache4_decode": (ctypes.c_int, [ctypes.POINTER(GmcCache4), _vp, _i64, _f32, _i64, _i64, _vp, _vp, _vp, _i64,
+                                         _vp]),
     "gmc_workspace_bytes": (_i64, []),
     "gmc_last_error": (ctypes.c_char_p, []),
     "gmc_free": (None, []),
@@ -458,6 +483,42 @@ def gmc_cache_evict(cache: GmcCache, budget, sinks, recent, workspace, workspace
     return lib().gmc_cache_evict(ctypes.byref(cache), budget, sinks, recent, workspace, workspace_bytes, stream)
 
 
+def gmc_cache_append_rotary(cache: GmcCache, rotary: GmcRotary, k, v, k_stride, v_stride, rows, starts, src, max_new,
+                            pos, q, q_stride, q_out, stream=None) -> int:
+    return lib().gmc_cache_append_rotary(ctypes.byref(cache), ctypes.byref(rotary), k, v, k_stride, v_stride, rows,
+                                         starts, src, max_new, pos, q, q_stride, q_out, stream)
+
+
+def gmc_cache4_append(cache: GmcCache4, rotary, k, v, k_stride, v_stride, rows, starts, src, max_new, pos, q,
+                      q_stride, q_out, stream=None) -> int:
+    return lib().gmc_cache4_append(ctypes.byref(cache), None if rotary is None else ctypes.byref(rotary), k, v,
+                                   k_stride, v_stride, rows, starts, src, max_new, pos, q, q_stride, q_out, stream)
+
+
+def gmc_cache4_read(cache: GmcCache4, rows, starts, max_new, k_out, v_out, stream=None) -> int:
+    return lib().gmc_cache4_read(ctypes.byref(cache), rows, starts, max_new, k_out, v_out, stream)
+
+
+def gmc_cache4_prefill_bytes(cache: GmcCache4, max_new: int) -> int:
+    return lib().gmc_cache4_prefill_bytes(ctypes.byref(cache), max_new)
+
+
+def gmc_cache4_prefill(cache: GmcCache4, q, q_stride, rows, starts, max_new, scale, window, sinks, out, lse, workspace,
+                       workspace_bytes, stream=None) -> int:
+    return lib().gmc_cache4_prefill(ctypes.byref(cache), q, q_stride, rows, starts, max_new, scale, window, sinks, out,
+                                    lse, workspace, workspace_bytes, stream)
+
+
+def gmc_cache4_decode_bytes(cache: GmcCache4) -> int:
+    return lib().gmc_cache4_decode_bytes(ctypes.byref(cache))
+
+
+def gmc_cache4_decode(cache: GmcCache4, q, q_stride, scale, window, sinks, out, lse, workspace, workspace_bytes,
+                      stream=None) -> int:
+    return lib().gmc_cache4_decode(ctypes.byref(cache), q, q_stride, scale, window, sinks, out, lse, workspace,
+                                   workspace_bytes, stream)
+
+
 def gmc_workspace_bytes() -> int:
     return int(lib().gmc_workspace_bytes())
 
@@ -669,6 +730,47 @@ def check_cache_tensors(k_pages, v_pages, page_table, lens, n_q_heads, slot_pos=
             raise ValueError(f"{name} must be on the GPU, on k_pages' device; got {x.device}")
 
 
+class Rotary:
+    """The table of a rotary position encoding (gmc_rotary), which it keeps alive.
+
+    ``cos`` / ``sin`` [n_pos][rot_dim / 2] float32 on the GPU: of the angle of each
+    pair at each position.  ``interleaved``: a pair is two neighbouring elements,
+    not one of each half.  ``sections`` (t, h, w): how many pairs, in this order,
+    turn by each of a token's three positions.
+    """
+
+    def __init__(self, cos, sin, *, interleaved=False, sections=None):
+        import torch
+        if cos.dim() != 2 or cos.dtype != torch.float32 or cos.shape != sin.shape or sin.dtype != torch.float32:
+            raise ValueError("cos and sin must be float32 [n_pos][rot_dim / 2] of one shape, got "
+                             f"{cos.dtype} {tuple(cos.shape)} and {sin.dtype} {tuple(sin.shape)}")
+        if cos.shape[0] < 1 or cos.shape[1] < 8 or cos.shape[1] % 8 != 0:
+            raise ValueError(f"rot_dim={2 * cos.shape[1]} must be a positive multiple of 16, with at least one position")
+        if not cos.is_contiguous() or not sin.is_contiguous():
+            raise ValueError("cos and sin must be contiguous")
+        if cos.device.type != "cuda" or sin.device != cos.device:
+            raise ValueError(f"cos and sin must be on one GPU; got {cos.device} and {sin.device}")
+        if sections is not None:
+            sections = tuple(int(n) for n in sections)
+            if len(sections) != 3 or any(n < 0 or n % 4 for n in sections) or sum(sections) != cos.shape[1]:
+                raise ValueError(f"sections={sections} must be three multiples of 4 that hold {cos.shape[1]} pairs")
+        self.cos, self.sin, self.sections, self.device = cos, sin, sections, cos.device
+        self.desc = GmcRotary(cos.data_ptr(), sin.data_ptr(), cos.shape[0], 2 * cos.shape[1], int(bool(interleaved)),
+                              (_i32 * 3)(*(sections or (0, 0, 0))))
+        self._ref = ctypes.byref(self.desc)
+
+    @classmethod
+    def create(cls, n_pos, rot_dim, *, base=10000.0, device="cuda", **more):
+        """The angles position * base ** (-2 j / rot_dim) of pairs j, formed in
+        64 bits (at position 10^5 the first pair's would be off by 4e-3 in 32)."""
+        import torch
+        if n_pos < 1 or rot_dim < 16 or rot_dim % 16 != 0:
+            raise ValueError(f"n_pos={n_pos} must be at least 1 and rot_dim={rot_dim} a positive multiple of 16")
+        f = float(base) ** (-torch.arange(0, rot_dim, 2, dtype=torch.float64, device=device) / rot_dim)
+        angle = torch.arange(n_pos, dtype=torch.float64, device=device)[:, None] * f
+        return cls(torch.cos(angle).float(), torch.sin(angle).float(), **more)
+
+
 class KvCache:
     """One layer's paged K/V cache of a batch of sequences (gmc_cache): the
     tensors, which the wrapper keeps alive, and the calls on them on torch's
@@ -684,28 +786,32 @@ class KvCache:
     """
 
     def __init__(self, k_pages, v_pages, page_table, lens, *, n_q_heads, slot_pos=None, seen=None, weights=None):
-        import torch
         check_cache_tensors(k_pages, v_pages, page_table, lens, n_q_heads, slot_pos, seen, weights)
-        self.torch = torch
-        self.k_pages, self.v_pages, self.page_table, self.lens = k_pages, v_pages, page_table, lens
+        self.k_pages, self.v_pages = k_pages, v_pages
         self.slot_pos, self.seen, self.weights = slot_pos, seen, weights
-        self.device, self.dtype = k_pages.device, k_pages.dtype
         n_pages, hkv, page, dh = k_pages.shape
+        ptr = (lambda t: None if t is None else t.data_ptr())
+        self._start(k_pages.device, k_pages.dtype, page_table, lens, n_q_heads, hkv, page, dh)
+        self.desc = GmcCache(GMC_BF16 if self.dtype == self.torch.bfloat16 else GMC_F32, n_q_heads, hkv, dh, page,
+                             page_table.shape[1], n_pages, self.n_seq, ptr(k_pages), ptr(v_pages), ptr(page_table),
+                             ptr(lens), ptr(seen), ptr(slot_pos), ptr(weights))
+        self._ref = ctypes.byref(self.desc)
+
+    _kind = "gmc_cache_"    # what the names of its entry points begin with
+
+    def _start(self, device, dtype, page_table, lens, n_q_heads, hkv, page, dh):
+        import torch
+        self.torch, self.device, self.dtype, self.page_table, self.lens = torch, device, dtype, page_table, lens
         self.n_seq, self.slots = page_table.shape[0], page_table.shape[1] * page
         self.n_q_heads, self.n_kv_heads, self.head_dim = n_q_heads, hkv, dh
-        ptr = (lambda t: None if t is None else t.data_ptr())
         self._scale = dh ** -0.5
         self._index_of_device = self.device.index
         self._current_device = torch.cuda.current_device
         # (the address alone: a Stream object takes longer than the call)
         self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
             (lambda i: torch.cuda.current_stream(i).cuda_stream)
-        self._entry = {n: getattr(lib(), n) for n in SIGNATURES if n.startswith("gmc_cache_")}
+        self._entry = {n: getattr(lib(), n) for n in SIGNATURES if n.startswith(self._kind)}
         self._need = {}
-        self.desc = GmcCache(GMC_BF16 if self.dtype == torch.bfloat16 else GMC_F32, n_q_heads, hkv, dh, page,
-                             page_table.shape[1], n_pages, self.n_seq, ptr(k_pages), ptr(v_pages), ptr(page_table),
-                             ptr(lens), ptr(seen), ptr(slot_pos), ptr(weights))
-        self._ref = ctypes.byref(self.desc)
 
     @classmethod
     def create(cls, *, n_seq, slots, n_q_heads, n_kv_heads, head_dim, dtype, device="cuda", page_size=64,
@@ -737,12 +843,12 @@ class KvCache:
         if code != GMC_OK:
             _check(code, name)
 
-    def _scratch(self, name, what):
+    def _scratch(self, name, *what):
         """(tensor or None, its address, its bytes) for a call; sizes are asked for
         once for each `what`, the memory is torch's, of the call's own."""
         need = self._need.get((name, what))
         if need is None:
-            need = self._entry[name + "_bytes"](self._ref, what)
+            need = self._entry[name + "_bytes"](self._ref, *what)
             if need < 0:
                 _check(int(need), name)
             self._need[name, what] = need
@@ -783,6 +889,10 @@ class KvCache:
         """gmc_cache_append: k, v [tokens][n_kv_heads][head_dim] (tokens may be
         strided); ``starts`` [n_seq + 1] int32 with ``max_new`` for ragged
         rows, or ``src`` [n_seq][n] int32, the rows of each sequence to take."""
+        self._call("gmc_cache_append", *self._appended(k, v, starts, max_new, src))
+
+    def _appended(self, k, v, starts, max_new, src):
+        """Addresses of k and v, their strides, rows, addresses of starts and src, max_new."""
         sk, sv = self._rows("k", k, self.n_kv_heads), self._rows("v", v, self.n_kv_heads)
         rows = k.shape[0]
         if v.shape[0] != rows:
@@ -796,7 +906,35 @@ class KvCache:
             first, max_new, taken = None, n, self._index("src", src, (self.n_seq, n))
         else:
             (first, max_new), taken = self._new(rows, starts, max_new), None
-        self._call("gmc_cache_append", k.data_ptr(), v.data_ptr(), sk, sv, rows, first, taken, max_new)
+        return k.data_ptr(), v.data_ptr(), sk, sv, rows, first, taken, max_new
+
+    def append_rotary(self, k, v, rotary, *, pos=None, q=None, starts=None, max_new=None, src=None, out=None):
+        """gmc_cache_append_rotary: append with k rotated by ``rotary`` (a Rotary)
+        on the way.  ``pos`` int32 [tokens], or [tokens][3] where the rotary has
+        sections; None: the slots' positions.  ``q`` [tokens][n_q_heads][head_dim]:
+        the tokens' queries; their rotated ones are returned (in ``out`` if given,
+        which without src may be q), [n_seq * n][n_q_heads][head_dim] with src."""
+        rows = self._appended(k, v, starts, max_new, src)
+        if rotary.device != self.device:
+            raise ValueError(f"rotary must be on the cache's device {self.device}; got {rotary.device}")
+        p = None if pos is None else self._index("pos", pos, (rows[4], 3) if rotary.sections else (rows[4],))
+        if q is None:
+            if out is not None:
+                raise ValueError("out needs q")
+            self._call(self._kind + self._turned, rotary._ref, *rows, p, None, 0, None)
+            return None
+        stride = self._rows("q", q, self.n_q_heads)
+        if q.shape[0] != rows[4]:
+            raise ValueError(f"q and k hold {q.shape[0]} and {rows[4]} tokens")
+        shape = (rows[4] if src is None else self.n_seq * rows[7], self.n_q_heads, self.head_dim)
+        if out is None:
+            out = self.torch.empty(shape, dtype=self.dtype, device=self.device)
+        elif tuple(out.shape) != shape or out.dtype != self.dtype or not out.is_contiguous() or out.device != self.device:
+            raise ValueError(f"out must be a contiguous {self.dtype} {shape} tensor on the cache's device")
+        self._call(self._kind + self._turned, rotary._ref, *rows, p, q.data_ptr(), stride, out.data_ptr())
+        return out
+
+    _turned = "append_rotary"
 
     def _outputs(self, q, out, lse):
         torch = self.torch
@@ -822,8 +960,8 @@ class KvCache:
         stride = self._rows("q", q, self.n_q_heads)
         first, max_new = self._new(q.shape[0], starts, max_new)
         out, ls = self._outputs(q, out, lse)
-        ws, at, size = self._scratch("gmc_cache_prefill", max_new)
-        self._call("gmc_cache_prefill", q.data_ptr(), stride, q.shape[0], first, max_new,
+        ws, at, size = self._scratch(self._kind + "prefill", max_new)
+        self._call(self._kind + "prefill", q.data_ptr(), stride, q.shape[0], first, max_new,
                    self._scale if scale is None else scale, window, sinks, out.data_ptr(),
                    None if ls is None else ls.data_ptr(), at, size)
         return out if ls is None else (out, ls)
@@ -846,6 +984,121 @@ class KvCache:
         head, the first ``sinks`` and last ``recent`` positions among them."""
         ws, at, size = self._scratch("gmc_cache_evict", budget)
         self._call("gmc_cache_evict", budget, sinks, recent, at, size)
+
+
+def check_cache4_tensors(k_codes, v_codes, k_scales, v_scales, page_table, lens, n_q_heads, dtype):
+    """Shapes, dtypes and devices of the tensors of a cache of 4 bits (see
+    gmc_cache4).  Raises ValueError."""
+    import torch
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"dtype must be float32 or bfloat16, got {dtype}")
+    if k_codes.dim() != 4 or k_codes.dtype != torch.uint8 or k_codes.shape[3] < 16 or k_codes.shape[3] % 16 != 0:
+        raise ValueError("k_codes must be uint8 [n_pages][n_kv_heads][page_size][head_dim / 2], head_dim a multiple of "
+                         f"32, got {k_codes.dtype} {tuple(k_codes.shape)}")
+    if v_codes.shape != k_codes.shape or v_codes.dtype != torch.uint8:
+        raise ValueError("v_codes must have k_codes' shape and dtype")
+    want = tuple(k_codes.shape[:3]) + (cache4_scale_bytes(2 * k_codes.shape[3]),)
+    for name, x in (("k_scales", k_scales), ("v_scales", v_scales)):
+        if tuple(x.shape) != want or x.dtype != torch.uint8:
+            raise ValueError(f"{name} must be uint8 {want}, got {x.dtype} {tuple(x.shape)}")
+    if page_table.dim() != 2 or page_table.dtype != torch.int32:
+        raise ValueError("page_table must be int32 [n_seq][max_pages]")
+    if k_codes.numel() == 0 or page_table.numel() == 0:
+        raise ValueError(f"k_codes {tuple(k_codes.shape)} and page_table {tuple(page_table.shape)} must not be empty")
+    if n_q_heads < 1 or n_q_heads % k_codes.shape[1] != 0:
+        raise ValueError(f"n_q_heads={n_q_heads} must be a multiple of the cache's {k_codes.shape[1]} kv heads")
+    if tuple(lens.shape) != (page_table.shape[0],) or lens.dtype != torch.int32:
+        raise ValueError(f"lens must be int32 [n_seq] = ({page_table.shape[0]},)")
+    tensors = [("k_codes", k_codes), ("v_codes", v_codes), ("k_scales", k_scales), ("v_scales", v_scales),
+               ("page_table", page_table), ("lens", lens)]
+    for name, x in tensors:
+        if not x.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+    for name, x in tensors:
+        if x.device.type != "cuda" or x.device != k_codes.device:
+            raise ValueError(f"{name} must be on the GPU, on k_codes' device; got {x.device}")
+
+
+def cache4_scale_bytes(head_dim):
+    """Bytes of the scales of a row of a cache of 4 bits."""
+    return 1 << (head_dim // 32 - 1).bit_length()
+
+
+class KvCache4(KvCache):
+    """One layer's paged K/V cache of a batch of sequences in 4 bits, 4.25 with
+    the scales (gmc_cache4): KvCache's calls but evict, and read.
+
+    ``k_codes`` / ``v_codes`` [n_pages][n_kv_heads][page_size][head_dim / 2] uint8,
+    ``k_scales`` / ``v_scales`` [n_pages][n_kv_heads][page_size][head_dim / 32,
+    rounded up to a power of two] uint8, ``page_table`` and ``lens`` as KvCache's;
+    ``dtype`` is that of k, v, q and the outputs.  Sharing pages as with KvCache.
+    """
+
+    def __init__(self, k_codes, v_codes, k_scales, v_scales, page_table, lens, *, n_q_heads, dtype):
+        check_cache4_tensors(k_codes, v_codes, k_scales, v_scales, page_table, lens, n_q_heads, dtype)
+        self.k_codes, self.v_codes, self.k_scales, self.v_scales = k_codes, v_codes, k_scales, v_scales
+        n_pages, hkv, page, half = k_codes.shape
+        self._start(k_codes.device, dtype, page_table, lens, n_q_heads, hkv, page, 2 * half)
+        self.desc = GmcCache4(GMC_BF16 if dtype == self.torch.bfloat16 else GMC_F32, n_q_heads, hkv, 2 * half, page,
+                              page_table.shape[1], n_pages, self.n_seq,
+                              *(x.data_ptr() for x in (k_codes, v_codes, k_scales, v_scales, page_table, lens)))
+        self._ref = ctypes.byref(self.desc)
+
+    _kind = "gmc_cache4_"
+    _turned = "append"
+
+    @classmethod
+    def create(cls, *, n_seq, slots, n_q_heads, n_kv_heads, head_dim, dtype, device="cuda", page_size=64):
+        """An empty cache of `slots` slots a sequence (rounded up to whole
+        pages), its pages in order."""
+        import torch
+        if n_seq < 1 or slots < 1 or page_size < 1:
+            raise ValueError(f"n_seq={n_seq}, slots={slots} and page_size={page_size} must be at least 1")
+        if head_dim < 32 or head_dim % 32 != 0:
+            raise ValueError(f"head_dim={head_dim} must be a positive multiple of 32")
+        per = -(-slots // page_size)
+        rows = (n_seq * per, n_kv_heads, page_size)
+        new = [torch.zeros(rows + (n,), dtype=torch.uint8, device=device)
+               for n in (head_dim // 2, head_dim // 2, cache4_scale_bytes(head_dim), cache4_scale_bytes(head_dim))]
+        table = torch.arange(n_seq * per, dtype=torch.int32, device=device).view(n_seq, per)
+        lens = torch.zeros(n_seq, dtype=torch.int32, device=device)
+        return cls(*new, table, lens, n_q_heads=n_q_heads, dtype=dtype)
+
+    def append(self, k, v, *, starts=None, max_new=None, src=None):
+        """gmc_cache4_append without rotation: as KvCache.append, each block of 32
+        elements to the nearest values of 4 bits and a power of two."""
+        self._call("gmc_cache4_append", None, *self._appended(k, v, starts, max_new, src), None, None, 0, None)
+
+    def read(self, rows=None, *, starts=None, max_new=None):
+        """gmc_cache4_read: the newest slots' values as (k, v) [tokens][n_kv_heads]
+        [head_dim], ``max_new`` of each sequence, or ragged by ``starts`` in
+        tensors of ``rows`` rows (those of no sequence are not written)."""
+        if starts is None:
+            if max_new is None or (rows is not None and rows != self.n_seq * max_new):
+                raise ValueError(f"without starts read needs max_new, and rows={rows} must be n_seq * max_new or not given")
+            rows = self.n_seq * max_new
+        elif rows is None:
+            raise ValueError("starts needs rows, the rows of the outputs")
+        if rows < 1:
+            raise ValueError(f"rows={rows} must be at least 1")
+        first, max_new = self._new(rows, starts, max_new)
+        k, v = (self.torch.empty((rows, self.n_kv_heads, self.head_dim), dtype=self.dtype, device=self.device) for _ in "kv")
+        self._call("gmc_cache4_read", rows, first, max_new, k.data_ptr(), v.data_ptr())
+        return k, v
+
+    def decode(self, q, *, window=0, sinks=0, scale=None, lse=False, out=None):
+        """gmc_cache4_decode: as KvCache.decode; no weights are accumulated."""
+        stride = self._rows("q", q, self.n_q_heads)
+        if q.shape[0] != self.n_seq:
+            raise ValueError(f"q must hold one token for each of {self.n_seq} sequences, got {q.shape[0]}")
+        out, ls = self._outputs(q, out, lse)
+        ws, at, size = self._scratch("gmc_cache4_decode")
+        self._call("gmc_cache4_decode", q.data_ptr(), stride, self._scale if scale is None else scale, window, sinks,
+                   out.data_ptr(), None if ls is None else ls.data_ptr(), at, size)
+        return out if ls is None else (out, ls)
+
+    def evict(self, budget, *, sinks=0, recent=0):
+        raise TypeError("a cache of 4 bits keeps its rows: slots have no weights and positions to evict by")
 
 
 def gmc_timing_enable(enable: bool) -> int:

@@ -45,6 +45,33 @@ struct AttendArgs {
   float* lse;             // [rows][hq] or null
 };
 
+// The scales of a cache of 4 bits, whose view holds its codes as k and v: a byte
+// for each 32 elements of a row, `bytes` to a row (a power of two).
+struct CacheScales {
+  uint8_t* k;
+  uint8_t* v;
+  int bytes;
+};
+constexpr int scale_bytes(int dh) { return dh <= 32 ? 1 : dh <= 64 ? 2 : dh <= 128 ? 4 : 8; }
+
+// A rotary table; pairs below t_end turn by the first of a token's `axes`
+// positions, those below h_end by the second, the others by the third.
+struct RotaryView {
+  const float* cos;       // [n_pos][rot / 2]
+  const float* sin;
+  int n_pos, rot, interleaved;
+  int axes, t_end, h_end;
+};
+
+// New rows of K and V, with the queries of their tokens.
+struct RotaryArgs {
+  const void *k, *v, *q;  // q may be null
+  long long k_stride, v_stride, q_stride, rows;   // strides in elements
+  const int32_t *starts, *src, *pos;
+  int max_new;
+  void* q_out;
+};
+
 #ifdef __HIPCC__
 // Four integers of an array that is aligned as one is.
 typedef int32_t i32x4_any __attribute__((ext_vector_type(4), aligned(4)));
@@ -116,5 +143,23 @@ hipError_t launch_cache_decode(const CacheView& c, const AttendArgs& a, bool acc
 long long evict_max_groups(const CacheView& c);
 long long evict_scratch_bytes(const CacheView& c);
 hipError_t launch_cache_evict(const CacheView& c, int budget, int sinks, int recent, void* scratch, hipStream_t st);
+
+// After every row has found its slot: the lengths (and positions given out).
+hipError_t launch_cache_advance(const CacheView& c, const int32_t* starts, long long rows, int max_new,
+                                hipStream_t st);
+
+// Appending with rotation; into 4 bits with scales.  rotary: null for none, then
+// into 4 bits only.
+hipError_t launch_cache_append_rotary(const CacheView& c, const CacheScales* scales, const RotaryView* rotary,
+                                      const RotaryArgs& a, hipStream_t st);
+
+// Caches of 4 bits.
+hipError_t launch_cache4_read(const CacheView& c, const CacheScales& s, long long rows, const int32_t* starts,
+                              int max_new, void* k_out, void* v_out, hipStream_t st);
+hipError_t launch_cache4_prefill(const CacheView& c, const CacheScales& s, const AttendArgs& a, void* scratch,
+                                 hipStream_t st);
+long long decode4_scratch_bytes(const CacheView& c);
+hipError_t launch_cache4_decode(const CacheView& c, const CacheScales& s, const AttendArgs& a, void* scratch,
+                                hipStream_t st);
 
 }  // namespace gmc

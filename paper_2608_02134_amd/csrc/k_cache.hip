@@ -83,16 +83,23 @@ __global__ void __launch_bounds__(256) cache_append_kernel(CacheView c, AppendAr
 }
 
 // After every row has found its slot: the lengths.
-__global__ void __launch_bounds__(256) cache_advance_kernel(CacheView c, AppendArgs a) {
+__global__ void __launch_bounds__(256) cache_advance_kernel(CacheView c, const int32_t* starts, int max_new,
+                                                             long long rows) {
   const int b = blockIdx.x * 256 + threadIdx.x;
   if (b >= c.n_seq) return;
   long long first;
   int n;
-  new_rows(a.starts, a.max_new, a.rows, b, &first, &n);
+  new_rows(starts, max_new, rows, b, &first, &n);
   const int len = cache_len(c, b);
   n = min(n, c.cap - len);
   c.lens[b] = len + n;
   if (c.seen) c.seen[b] += n;
+}
+
+hipError_t launch_cache_advance(const CacheView& c, const int32_t* starts, long long rows, int max_new,
+                                hipStream_t st) {
+  hipLaunchKernelGGL(cache_advance_kernel, dim3((c.n_seq + 255) / 256), dim3(256), 0, st, c, starts, max_new, rows);
+  return hipGetLastError();
 }
 
 hipError_t launch_cache_append(const CacheView& c, const void* k, const void* v, long long k_stride,
@@ -107,7 +114,7 @@ hipError_t launch_cache_append(const CacheView& c, const void* k, const void* v,
     hipLaunchKernelGGL(cache_append_kernel, dim3(std::min((max_new + 3) / 4, 4096), c.n_seq), dim3(256), 0, st, c, a);
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;   // (rows that were not written are not counted)
-    hipLaunchKernelGGL(cache_advance_kernel, dim3((c.n_seq + 255) / 256), dim3(256), 0, st, c, a);
+    return launch_cache_advance(c, starts, rows, max_new, st);
   }
   return hipGetLastError();
 }

@@ -30,54 +30,13 @@
 #include <algorithm>
 
 #include "gmc_cache.h"
+#include "gmc_decode.h"
 #include "gmc_device.h"
 
 namespace gmc {
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr int kDecodeWaves = 4, kDecodeShort = 8;   // waves of a block; where one block does a whole sequence
-
 // Keys a wave takes at a time.
 template <typename T> constexpr int kHalves = sizeof(T) == 2 ? 2 : 1;
-
-// Which tiles of TK slots a query in slot t looks at: all up to its own, or
-// with a window over slots in order those of the first tokens and the window.
-struct TileRange {
-  int first, skip, count;   // tile i: i < first ? i : i + skip
-};
-__host__ __device__ inline TileRange tile_range(int len, int window, int sinks, bool ordered, int tk) {
-  TileRange r;
-  const int end = (len + tk - 1) / tk;
-  if (window <= 0 || !ordered || window >= len) {
-    r.first = end; r.skip = 0; r.count = end;
-    return r;
-  }
-  const int lo = (len - window) / tk;
-  const int sink = (sinks < len ? sinks + tk - 1 : len + tk - 1) / tk;
-  r.first = sink < lo ? sink : lo;
-  r.skip = lo - r.first;
-  r.count = end - r.skip;
-  return r;
-}
-
-struct DecodeScratch {
-  float* part;     // [b][hq][nsplit][dh] unnormalised sums
-  float* ml;       // [b][hq][nsplit][2] maximum (base 2) and sum
-  float* logits;   // [b][hq][cap] or null
-  int nsplit;
-};
-
-// Splits that a sequence's tiles are shared over, at most those of the grid:
-// one tile a wave up to 32 splits, above that two, above 64 four, as the join
-// reads every split (28 query heads on 4, bf16; one request of 32768 slots:
-// 20.2 us with 64 splits, 22.1 with 128, 30 with 256; of 4096: 9.2 with 32,
-// 10.5 with 16).
-__host__ __device__ inline int used_splits(int tiles, int nsplit) {
-  const int one = (tiles + kDecodeWaves - 1) / kDecodeWaves;
-  const int two = (one + 1) / 2, four = (two + 1) / 2;
-  const int want = one < 32 ? one : two < 32 ? 32 : two < 64 ? two : four < 64 ? 64 : four;
-  return nsplit < want ? nsplit : want < 1 ? 1 : want;
-}
 
 template <int N> struct Raw;
 template <> struct Raw<1> { uint32_t u[1]; };
@@ -436,6 +395,16 @@ decode_join_kernel(CacheView c, AttendArgs a, DecodeScratch sc, int tk) {
     if (s + u < len) to[u] += add[u];
 }
 
+hipError_t launch_decode_join(const CacheView& c, const AttendArgs& a, const DecodeScratch& sc, bool accumulate, int tk,
+                              hipStream_t st) {
+  const dim3 grid(c.hg + (accumulate ? (c.cap + 1023) / 1024 : 0), c.hkv, c.n_seq);
+  if (c.dtype == 0)
+    hipLaunchKernelGGL(decode_join_kernel<float>, grid, dim3(256), 0, st, c, a, sc, tk);
+  else
+    hipLaunchKernelGGL(decode_join_kernel<bf16_t>, grid, dim3(256), 0, st, c, a, sc, tk);
+  return hipGetLastError();
+}
+
 // Splits of a call: enough blocks for the chip (64 requests of 4096 slots:
 // 51.6 us with 1024 blocks, 57 with 2048, 70 with 4096).
 static int decode_splits(const CacheView& c, int qtiles) {
@@ -501,12 +470,7 @@ hipError_t launch_cache_decode(const CacheView& c, const AttendArgs& a, bool acc
   const hipError_t err =
       c.dtype == 0 ? start_decode<float>(c, a, sc, qt, one_block, st) : start_decode<bf16_t>(c, a, sc, qt, one_block, st);
   if (err != hipSuccess || !join) return err;
-  const dim3 jgrid(c.hg + (accumulate ? (c.cap + 1023) / 1024 : 0), c.hkv, c.n_seq);
-  if (c.dtype == 0)
-    hipLaunchKernelGGL(decode_join_kernel<float>, jgrid, dim3(256), 0, st, c, a, sc, tk);
-  else
-    hipLaunchKernelGGL(decode_join_kernel<bf16_t>, jgrid, dim3(256), 0, st, c, a, sc, tk);
-  return hipGetLastError();
+  return launch_decode_join(c, a, sc, accumulate, tk, st);
 }
 
 }  // namespace gmc

@@ -1,0 +1,41 @@
+// Attention of the newest tokens of each sequence over a paged cache of 4 bits.
+//
+// The products are those over pages of the type (k_prefill.hip): a tile of keys in
+// shared memory serves 128 rows, so its values are formed once, between the pages
+// and shared memory, and the codes of the next tile are on their way in registers
+// (8 a thread) meanwhile.  bf16 holds every value exactly; fp32 products take the
+// values as fp32.
+#include "gmc_prefill.h"
+
+namespace gmc {
+
+template <typename T, int DH>
+__global__ void __launch_bounds__(64 * kPreWaves, sizeof(T) == 2 && DH <= 128 ? 2 : 1)
+prefill4_kernel(CacheView c, CacheScales s, AttendArgs a, PreScratch sc, int row_blocks) {
+  prefill_block<T, DH, true>(c, s, a, sc, row_blocks);
+}
+
+hipError_t launch_cache4_prefill(const CacheView& c, const CacheScales& s, const AttendArgs& a, void* scratch,
+                                 hipStream_t st) {
+  int row_blocks;
+  const PreScratch sc = pre_plan(c, a.max_new, scratch, &row_blocks);
+#define GMC_PREFILL4(T, DH)                                                                                       \
+  case DH:                                                                                                        \
+    hipLaunchKernelGGL((prefill4_kernel<T, DH>), dim3(static_cast<unsigned>(sc.grid.blocks)), dim3(64 * kPreWaves), 0, st, \
+                       c, s, a, sc, row_blocks);                                                                  \
+    break;
+#define GMC_PREFILL4_ALL(T)                                                                                       \
+  switch (c.dh) {                                                                                                 \
+    GMC_PREFILL4(T, 32) GMC_PREFILL4(T, 64) GMC_PREFILL4(T, 96) GMC_PREFILL4(T, 128)                              \
+    GMC_PREFILL4(T, 160) GMC_PREFILL4(T, 192) GMC_PREFILL4(T, 224) GMC_PREFILL4(T, 256)                           \
+    default: return hipErrorInvalidValue;                                                                         \
+  }
+  if (c.dtype == 0) { GMC_PREFILL4_ALL(float) } else { GMC_PREFILL4_ALL(bf16_t) }
+#undef GMC_PREFILL4_ALL
+#undef GMC_PREFILL4
+  const hipError_t err = hipGetLastError();
+  if (err != hipSuccess) return err;   // (there is nothing to join)
+  return sc.nsplit > 1 ? launch_prefill_join(c, a, sc, st) : hipSuccess;
+}
+
+}  // namespace gmc
