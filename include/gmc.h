@@ -710,7 +710,8 @@ int gmc_cache_append_rotary(const gmc_cache* cache, const gmc_rotary* rotary, co
  * a byte e for 2^(e - 127) (255: the block reads as NaN), and 32 codes of 4 bits:
  * bit 3 is the sign, bits 2..0 number the magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6.
  * Byte i of a row's codes holds element 2 i in its lower half and 2 i + 1 in its
- * upper one.  A value is code times scale; each is a bfloat16 exactly.
+ * upper one.  A value is code times scale; up to 6 * 2^125, the largest that is
+ * appended, each is a bfloat16 exactly.
  *   k_codes, v_codes   [n_pages][n_kv_heads][page_size][head_dim / 2] bytes,
  *                      16-byte aligned
  *   k_scales, v_scales [n_pages][n_kv_heads][page_size][S] bytes, 16-byte
@@ -736,9 +737,10 @@ typedef struct gmc_cache4 {
 /*
  * gmc_cache4_append - gmc_cache_append, or gmc_cache_append_rotary with `rotary`
  * not NULL, into a cache of 4 bits.  A block's scale is the least power of two
- * from 2^-126 on for which no magnitude of the (rotated, fp32) block is above 7
- * scales, and each element becomes the nearest code, ties to the even one: off by
- * at most a quarter of the scale up to 2 scales, half up to 4, one above.  A block
+ * from 2^-126 to 2^125 for which no magnitude of the (rotated, fp32) block is above
+ * 7 scales, and each element becomes the nearest code, ties to the even one: off
+ * by at most a quarter of the scale up to 2 scales, half up to 4, one above.
+ * (Magnitudes above 7 * 2^125, near the largest number, become 6 * 2^125.)  A block
  * with an infinity or NaN gets scale 255.  Without rotary, pos, q and q_out must
  * be NULL.
  */

@@ -26,14 +26,15 @@ __device__ __forceinline__ uint4 fp4_words(uint32_t codes, float scale) {
 
 // The scale byte of a block whose largest magnitude has the bits `top`: the
 // least e >= 1 with top <= 7 * 2^(e - 127).  1.75 * 2^k is 7 * 2^(k - 2), so
-// what is left after the leading bit decides between k - 2 and k - 1.
+// what is left after the leading bit decides between k - 2 and k - 1.  At most
+// 252, whose 6 scales are the largest that does not overflow.
 __device__ __forceinline__ uint32_t fp4_scale(uint32_t top) {
   const int e = static_cast<int>((top + 0x1FFFFFu) >> 23) - 2;
-  return top >= 0x7F800000u ? 255u : static_cast<uint32_t>(max(e, 1));
+  return top >= 0x7F800000u ? 255u : static_cast<uint32_t>(min(max(e, 1), 252));
 }
 
-// Eight values as codes: nearest, ties to even; magnitudes above 6 scales (up to
-// 7) become 6.
+// Eight values as codes: nearest, ties to even; magnitudes above 6 scales become
+// 6.
 __device__ __forceinline__ uint32_t fp4_codes(const float* x, float scale) {
   uint32_t u = 0;
   u = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(u, x[0], x[1], scale, 0);

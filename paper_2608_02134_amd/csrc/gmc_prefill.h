@@ -588,12 +588,18 @@ __device__ __forceinline__ void prefill_block(const CacheView& c, const CacheSca
         if (row_at < 0) continue;
         const int p = pos ? pos[s] : s;
         const bool see = s <= t && (!a.window || mine - p < a.window || p < a.sinks);
-        if constexpr (Q4) {   // (a run of 32 is NaN or has none)
+        if constexpr (Q4) {   // (scales from 2^126 on, which nothing appends, overflow)
           const uint8_t* sp = s4.v + row_at * scale_bytes(DH);
+          const uint8_t* cp = static_cast<const uint8_t*>(c.v) + row_at * (DH / 2) + 2 * half;
 #pragma unroll
           for (int n = 0; n < NB; ++n)
+            if (see && sp[n] >= 253)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) o[n][i] += see && sp[n] == 255 ? __builtin_nanf("") : 0.f;
+              for (int i = 0; i < 16; ++i) {
+                const uint32_t code = cp[16 * n + 4 * (i >> 2) + ((i & 3) >> 1)] >> (4 * (i & 1));
+                const float v = __uint_as_float(fp4_pair<0>(code, scale_of(sp[n])) << 16);
+                o[n][i] += fabsf(v) < INFINITY ? 0.f : v;
+              }
           continue;
         }
         const T* vp = static_cast<const T*>(c.v) + row_at * DH + 4 * half;

@@ -216,11 +216,16 @@ decode4_kernel(CacheView c, CacheScales sc4, AttendArgs a, DecodeScratch sc, int
         if constexpr (NP == 2) {
           const uint32_t u = __float_as_uint(e) & 0xFFFF0000u;
           p[0][at] = __builtin_bit_cast(__bf16, static_cast<uint16_t>(u >> 16));
-          p[1][at] = static_cast<__bf16>(e - __uint_as_float(u));
+          // (no part of a weight above zero is zero: an infinite value, which
+          // scales from 2^126 on have, stays what it is)
+          p[1][at] = static_cast<__bf16>(fmaxf(e - __uint_as_float(u), e * 0x1p-24f));
         } else {
-          __bf16 x0, x1, x2;
-          split3(e, &x0, &x1, &x2);
-          p[0][at] = x0; p[1][at] = x1; p[2][at] = x2;
+          const uint32_t u = __float_as_uint(e) & 0xFFFF0000u;
+          const float rest = e - __uint_as_float(u);
+          const uint32_t v = __float_as_uint(fmaxf(rest, e * 0x1p-25f)) & 0xFFFF0000u;
+          p[0][at] = __builtin_bit_cast(__bf16, static_cast<uint16_t>(u >> 16));
+          p[1][at] = __builtin_bit_cast(__bf16, static_cast<uint16_t>(v >> 16));
+          p[2][at] = static_cast<__bf16>(fmaxf(rest - __uint_as_float(v), e * 0x1p-33f));
         }
       }
     l = l * f + sum;   // this lane group's keys; joined at the end
