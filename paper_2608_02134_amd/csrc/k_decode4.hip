@@ -1,20 +1,30 @@
 // Attention of one new token per sequence over a paged cache of 4 bits.
 //
 // As over pages of bf16 (S^T = K Q^T, O^T = V^T P^T, keys split over blocks and
-// joined by a second kernel), with codes and scales loaded from the pages and
-// turned into bf16 operands by single instructions, exactly.  136 bytes a row of
-// 128 elements for K and V instead of 512: bound by memory where the caches are long,
-// and the instructions beside it have to stay few:
+// joined by a second kernel), with 136 bytes a row of 128 elements for K and V instead
+// of 512: bound by memory where the caches are long, if enough loads are on their way
+// and the instructions beside them are few.
+//   Loads: tiles of 32 keys go from the pages into shared memory without registers
+//      between, each wave its own, two tiles ahead of the one it computes: five loads
+//      a tile of 128 dims.  (Into registers, 14 loads a tile, one tile ahead: 278 us where
+//      this takes 198; loads alone take 182.)  What a lane loads is what it reads back,
+//      where K is concerned; V is turned by the addresses of the reads.
 //   K: the order of the elements in a product is free, so lane (key l % 16, group g =
-//      l / 16) takes a run of them: of each 128 the 32 from 32 g, one 16-byte load and
-//      one scale; of what is left 16 from 16 g (64) and 8 from 8 g (32).
+//      l / 16) takes a run of them: of each 128 the 32 from 32 g, one block with one
+//      scale; of what is left 16 from 16 g (64) and 8 from 8 g (32).
 //   V: lane (i = l % 16, g) takes of each of its group's keys 4 g + 0..3 the 8
-//      elements from 8 i of each 128 (4 of 64, 2 of 32), whole rows over 16 lanes,
-//      and turns pairs of two keys into operands by byte permutations.
+//      elements from 8 i of each 128 (4 of 64, 2 of 32), and turns pairs of two keys
+//      into operands by byte permutations.
+//   Codes become bf16 by single instructions, exactly; a scale's byte comes to its
+//      place by one rotation.
 // Every value is a bf16, so fp32 queries and weights enter as three bf16 (24
 // bits: exact but for the last, which is rounded) and the products are those of
 // fp32; weights for bf16 outputs as two (16 bits).  The matrix cores idle, so this
 // costs nothing.
+//
+// 8 requests of 100000 to 131072 slots, 32 heads on 8 of 128 in bf16: 193 us, 5.2
+// TB/s (of bf16 pages 633).  64 requests of 200 to 4096 slots, 28 heads on 4: 26 us
+// with the joining kernel.
 #include <algorithm>
 
 #include "gmc_cache.h"
@@ -33,21 +43,15 @@ template <int DH> struct Runs {
   static constexpr int base(int n) { return n <= n128 ? 128 * n : 128 * n128 + 64; }
 };
 
-template <int N> __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t* u) {
-  static_assert(N == 1 || N == 2 || N == 4 || N == 8, "runs of 4 to 32 bytes");
-  if constexpr (N == 1) {
-    u[0] = *reinterpret_cast<const uint32_t*>(p);
-  } else if constexpr (N == 2) {
-    const uint2 v = *reinterpret_cast<const uint2*>(p);
-    u[0] = v.x; u[1] = v.y;
-  } else {
-#pragma unroll
-    for (int e = 0; e < N / 4; ++e) {
-      const uint4 v = reinterpret_cast<const uint4*>(p)[e];
-      u[4 * e] = v.x; u[4 * e + 1] = v.y; u[4 * e + 2] = v.z; u[4 * e + 3] = v.w;
-    }
-  }
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// Byte n of four as a scale: the conversions look at the exponent's bits alone, so
+// a rotation brings it there.
+__device__ __forceinline__ uint32_t scale_at_bits(uint32_t bytes, int n) {
+  return __builtin_amdgcn_alignbit(bytes, bytes, static_cast<uint32_t>(8 * n + 9) & 31u);
 }
+__device__ __forceinline__ float scale_at(uint32_t bytes, int n) { return __uint_as_float(scale_at_bits(bytes, n)); }
 
 // x as bf16 parts: the upper 8 significant bits, the next 8, and the rest rounded.
 // Infinities and NaN are all in the first part.
@@ -61,15 +65,57 @@ __device__ __forceinline__ void split3(float x, __bf16* hi, __bf16* mid, __bf16*
   *lo = static_cast<__bf16>(rest - m);
 }
 
+// Shared and global memory by their address spaces, as loads into shared memory
+// take them.
+typedef __attribute__((address_space(3))) uint8_t shared_u8;
+typedef __attribute__((address_space(1))) uint32_t global_u32;
+template <typename V> __device__ __forceinline__ V ld_shared(const shared_u8* p) {
+  return *reinterpret_cast<const __attribute__((address_space(3))) V*>(p);
+}
+
+// A tile in shared memory: 16-byte blocks of K, of V (whole loads of 64 of
+// them), then the rows' scales.  K's blocks stand block by block of the row, V's so
+// that the blocks that one read touches lie on different banks.
+template <int DH> struct Tile4 {
+  static constexpr int kBlocks = DH / 32, kLoads = (kBlocks + 1) / 2, kScaleBytes = scale_bytes(DH);
+  static constexpr int kScaleLoads = (kScaleBytes + 3) / 4;      // of 256 bytes
+  static constexpr int kV = 1024 * kLoads, kScales = 2 * kV, kBytes = kScales + 256 * kScaleLoads;
+  static constexpr int kInFlight = 2 * kLoads + kScaleLoads;     // loads of a tile
+  static __device__ __forceinline__ int k_at(int half, int row, int blk) { return 16 * ((half * kBlocks + blk) * 16 + row); }
+  static __device__ __forceinline__ int v_at(int half, int row, int blk) {
+    return kV + 16 * (half * 16 * kBlocks + ((row & 3) * 4 + (row >> 2)) * kBlocks + blk);
+  }
+  static __device__ __forceinline__ int scales_at(bool values, int half, int row) {
+    return kScales + (((values ? 2 : 0) + half) * 16 + row) * kScaleBytes;
+  }
+};
+
+template <int N> __device__ __forceinline__ void arrive() {   // until at most N loads are on their way
+  __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14));
+  asm volatile("" ::: "memory");
+}
+
+// Tiles a wave has in shared memory: the one it computes and those on their way.
+// Three blocks of four waves to a CU find room with heads of up to 128, two with
+// wider ones and in fp32 with 96 to 160, one in fp32 from 192 on, whose registers are
+// more.
+template <int DH, int WAVES> constexpr int kRing = DH <= 128 && WAVES == kDecodeWaves ? 3 : 2;
+constexpr int blocks_of_cu(int type_bytes, int dh, int waves) {
+  return type_bytes == 4 && dh > 160 ? 1 : dh <= (type_bytes == 2 ? 128 : 64) && waves == kDecodeWaves ? 3 : 2;
+}
 template <typename T, int DH, int WAVES>
-__global__ void __launch_bounds__(64 * WAVES)
+__global__ void __launch_bounds__(64 * WAVES, (blocks_of_cu(sizeof(T), DH, WAVES)))
 decode4_kernel(CacheView c, CacheScales sc4, AttendArgs a, DecodeScratch sc, int qtiles) {
   using R = Runs<DH>;
+  using L = Tile4<DH>;
   constexpr int H = 2, TK = kTile4, NS = DH / 32, NO = DH / 16, ROW = DH / 2;
-  constexpr int SB = scale_bytes(DH), SW = SB == 8 ? 2 : 1;
+  constexpr int SB = scale_bytes(DH);
   constexpr int NQ = sizeof(T) == 2 ? 1 : 3, NP = sizeof(T) == 2 ? 2 : 3;   // bf16 parts of queries and weights
-  __shared__ float red[WAVES / 2][16 * DH];
+  constexpr int kTiles = kRing<DH, WAVES>;
+  __shared__ __align__(16) uint8_t ring0[WAVES * L::kBytes], ring1[WAVES * L::kBytes];
+  __shared__ __align__(16) uint8_t ring2[kTiles > 2 ? WAVES * L::kBytes : 16];
   __shared__ float stat[WAVES][2][16];
+  static_assert(sizeof(ring0) >= WAVES / 2 * 16 * DH * sizeof(float), "the waves' parts take the first tiles' place");
   const int split = blockIdx.x, h = blockIdx.y / qtiles, qt = blockIdx.y % qtiles, b = blockIdx.z;
   const int lane = threadIdx.x & 63, w = wave_id(), i16 = lane & 15, g = lane >> 4;
   const int len = cache_len(c, b);
@@ -81,48 +127,69 @@ decode4_kernel(CacheView c, CacheScales sc4, AttendArgs a, DecodeScratch sc, int
   const int head = qt * 16 + i16;                 // of the group
   const bool live = head < c.hg;
   const int hq = h * c.hg + head;
-  const float scale = a.scale * kLog2e;
+  // exp2(scale log2(e) s): a negative scale goes to the queries' sign, and a
+  // scale of zero to the least one that does not turn a hidden key's -inf into NaN
+  const float cs = fmaxf(fabsf(a.scale) * kLog2e, 0x1p-149f);
+  const float slack = fminf(8.f / cs, 0x1p126f);   // (not infinite: the first maximum is above -inf + slack)
 
-  struct Tile {
-    uint32_t k[H][NS], v[H][4][R::count], sk[H][SW], sv[H][SB];
-    bool ok[H];             // the half tile is on a page
-    int slot0;
+  // (as constant memory, which nothing here writes: page ids come by scalar loads, and
+  // the vector loads on their way are those of tiles alone)
+  typedef const __attribute__((address_space(4))) int32_t constant_i32;
+  constant_i32* table = (constant_i32*)(c.table + static_cast<long long>(b) * c.max_pages);
+  auto slot0 = [&](int tile) { return (tile < tr.first ? tile : tile + tr.skip) * TK; };
+  // Page ids of a tile's halves; past the last tile as of it.
+  auto ids_of = [&](int tile, int* id) {
+    const int s = slot0(min(tile, t1 - 1));
+#pragma unroll
+    for (int hh = 0; hh < H; ++hh) id[hh] = table[min(s + 16 * hh, c.cap - 1) >> c.shift];
   };
-  const int32_t* table = c.table + static_cast<long long>(b) * c.max_pages;
-  auto load = [&](int tile, Tile& x) __attribute__((always_inline)) {
-    x.slot0 = (tile < tr.first ? tile : tile + tr.skip) * TK;
+  // Which halves of a tile are on a page: bits.
+  auto on_pages = [&](int tile, const int* id) {
+    unsigned ok = 0;
 #pragma unroll
-    for (int hh = 0; hh < H; ++hh) {
-      const int s = x.slot0 + 16 * hh;
-      long long row = 0;    // read and dropped where there is none
-      x.ok[hh] = s < len;
-      if (x.ok[hh]) {
-        const int id = table[s >> c.shift];
-        x.ok[hh] = id >= 0 && id < c.n_pages;
-        if (x.ok[hh]) row = ((static_cast<long long>(id) * c.hkv + h) << c.shift) + (s & (c.page - 1));
-      }
-      const uint8_t* kp = static_cast<const uint8_t*>(c.k) + row * ROW + i16 * ROW;
-      const uint8_t* vp = static_cast<const uint8_t*>(c.v) + row * ROW + 4 * g * ROW;
+    for (int hh = 0; hh < H; ++hh)
+      if (slot0(tile) + 16 * hh < len && id[hh] >= 0 && id[hh] < c.n_pages) ok |= 1u << hh;
+    return ok;
+  };
+  // Where a lane's scale words come from (K, K, V, V of 4 SB words each): kept, as
+  // the compiler would fetch the choice between the two anew, behind the loads on their way.
+  const uint8_t* scales_from[L::kScaleLoads];
+  bool second[L::kScaleLoads];
 #pragma unroll
-      for (int n = 0; n < R::count; ++n) {
-        constexpr int kWord = 32;   // elements of a group for each 128
-        const int at = R::base(n) / 2, size = R::size(n);
-        if (size == 128) load_words<4>(kp + at + 16 * g, &x.k[hh][R::base(n) / kWord]);
-        if (size == 64) load_words<2>(kp + at + 8 * g, &x.k[hh][R::base(n) / kWord]);
-        if (size == 32) load_words<1>(kp + at + 4 * g, &x.k[hh][R::base(n) / kWord]);
+  for (int u = 0; u < L::kScaleLoads; ++u) {
+    const int x = (64 * u + lane) % (16 * SB), part = x / (4 * SB);
+    const uint8_t *k = sc4.k, *v = sc4.v;
+    asm volatile("" : "+s"(k), "+s"(v));
+    scales_from[u] = ((part & 2) ? v : k) + 4 * (x - part * 4 * SB);
+    second[u] = part & 1;
+  }
+  // Loads a tile; rows that are none are those of the first page, and dropped.
+  auto issue = [&](int tile, const int* id, unsigned ok, shared_u8* to) __attribute__((always_inline)) {
+    // (pointers whose type depends on no template argument: clang drops the host's
+    // side of a kernel in which this builtin is only checked with its arguments)
+    shared_u8 *const values = to + L::kV, *const scales = to + L::kScales;
+    long long row[H];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const uint8_t* p = vp + r * ROW + at;
-          x.v[hh][r][n] = size == 128  ? *reinterpret_cast<const uint32_t*>(p + 4 * i16)
-                          : size == 64 ? *reinterpret_cast<const uint16_t*>(p + 2 * i16)
-                                       : p[i16];
-        }
-      }
-      const uint8_t* ks = sc4.k + row * SB + i16 * SB;
-      if constexpr (SB == 1) x.sk[hh][0] = *ks;
-      else if constexpr (SB == 2) x.sk[hh][0] = *reinterpret_cast<const uint16_t*>(ks);
-      else load_words<SB / 4>(ks, x.sk[hh]);
-      load_words<SB>(sc4.v + row * SB + 4 * g * SB, x.sv[hh]);
+    for (int hh = 0; hh < H; ++hh)
+      row[hh] = (ok >> hh) & 1u ? ((static_cast<long long>(id[hh]) * c.hkv + h) << c.shift) +
+                                      ((slot0(tile) + 16 * hh) & (c.page - 1))
+                                : 0;
+#pragma unroll
+    for (int u = 0; u < L::kLoads; ++u) {
+      // (the last load of an odd number of blocks takes some of them twice)
+      const int x = min(64 * u + lane, 32 * NS - 1), hh = x / (16 * NS), y = x - hh * 16 * NS;
+      const long long r = hh ? row[1] : row[0];
+      const int kr = y & 15, kblk = y >> 4;
+      const int vx = y / NS, vblk = y - vx * NS, vr = (vx & 3) * 4 + (vx >> 2);
+      const uint8_t* kp = static_cast<const uint8_t*>(c.k) + r * ROW + kr * ROW + 16 * kblk;
+      const uint8_t* vp = static_cast<const uint8_t*>(c.v) + r * ROW + vr * ROW + 16 * vblk;
+      __builtin_amdgcn_global_load_lds((const global_u32*)kp, to + 1024 * u, 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((const global_u32*)vp, values + 1024 * u, 16, 0, 0);
+    }
+#pragma unroll
+    for (int u = 0; u < L::kScaleLoads; ++u) {
+      const uint8_t* p = scales_from[u] + (second[u] ? row[1] : row[0]) * SB;
+      __builtin_amdgcn_global_load_lds((const global_u32*)p, scales + 256 * u, 4, 0, 0);
     }
   };
 
@@ -136,9 +203,14 @@ decode4_kernel(CacheView c, CacheScales sc4, AttendArgs a, DecodeScratch sc, int
         const int s = R::base(n) / 32 + u;
         const T* p = qp + R::base(n) + R::size(n) / 4 * g + 8 * u;
         if constexpr (sizeof(T) == 2) {
-          q[0][s] = live ? __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(p)) : bf16x8{};
+          uint4 y = live ? *reinterpret_cast<const uint4*>(p) : make_uint4(0u, 0u, 0u, 0u);
+          if (a.scale < 0.f) { y.x ^= 0x80008000u; y.y ^= 0x80008000u; y.z ^= 0x80008000u; y.w ^= 0x80008000u; }
+          q[0][s] = __builtin_bit_cast(bf16x8, y);
         } else {
-          const Frag<float> f = live ? frag_load<float>(p) : frag_zero<float>();
+          Frag<float> f = live ? frag_load<float>(p) : frag_zero<float>();
+          if (a.scale < 0.f)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f.v[e] = -f.v[e];
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
             __bf16 x0, x1, x2;
@@ -153,41 +225,53 @@ decode4_kernel(CacheView c, CacheScales sc4, AttendArgs a, DecodeScratch sc, int
   for (int n = 0; n < NO; ++n) o[n] = floatx4{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;
 
-  auto compute = [&](Tile& y) __attribute__((always_inline)) {
+  auto compute = [&](int tile, unsigned ok, const shared_u8* in) __attribute__((always_inline)) {
+    const int s0 = slot0(tile);
     // keys that are not seen: only in the last tile, at the window's edges and
     // on pages that are none
-    const bool whole = y.slot0 + TK <= len && (!a.window || len - 1 - y.slot0 < a.window) && y.ok[0] && y.ok[1];
+    const bool whole = s0 + TK <= len && (!a.window || len - 1 - s0 < a.window) && ok == 3u;
     floatx4 x[H];
 #pragma unroll
     for (int hh = 0; hh < H; ++hh) {
       x[hh] = floatx4{0.f, 0.f, 0.f, 0.f};
+      uint32_t sk[SB == 8 ? 2 : 1];
+      {
+        const shared_u8* p = in + L::scales_at(false, hh, i16);
+        if constexpr (SB == 1) sk[0] = *p;
+        else if constexpr (SB == 2) sk[0] = ld_shared<uint16_t>(p);
+        else if constexpr (SB == 4) sk[0] = ld_shared<uint32_t>(p);
+        else { const u32x2 y = ld_shared<u32x2>(p); sk[0] = y.x; sk[1] = y.y; }
+      }
 #pragma unroll
-      for (int n = 0; n < R::count; ++n)
+      for (int n = 0; n < R::count; ++n) {
+        const int blk = R::base(n) / 32, size = R::size(n);
+        // of 128 elements a group has a block, of 64 half of one, of 32 a quarter
+        const int mine = size == 128 ? g : size == 64 ? g >> 1 : 0;
+        const shared_u8* p = in + L::k_at(hh, i16, blk + mine);
+        uint32_t u[4];
+        if (size == 128) { const u32x4 y = ld_shared<u32x4>(p); u[0] = y.x; u[1] = y.y; u[2] = y.z; u[3] = y.w; }
+        if (size == 64) { const u32x2 y = ld_shared<u32x2>(p + 8 * (g & 1)); u[0] = y.x; u[1] = y.y; }
+        if (size == 32) u[0] = ld_shared<uint32_t>(p + 4 * g);
+        const float f = scale_at(sk[blk / 4], blk % 4 + mine);
 #pragma unroll
-        for (int u = 0; u < R::size(n) / 32; ++u) {
-          const int s = R::base(n) / 32 + u;
-          // block of the run's elements: of 128 one a group, of 64 one for two
-          const int blk = R::base(n) / 32, sh = R::size(n) == 128 ? 8 * g : R::size(n) == 64 ? 8 * (g >> 1) : 0;
-          const float f = scale_of((y.sk[hh][blk / 4] >> (8 * (blk % 4) + sh)) & 255u);
-          const bf16x8 kf = __builtin_bit_cast(bf16x8, fp4_words(y.k[hh][s], f));
+        for (int e = 0; e < size / 32; ++e) {
+          const bf16x8 kf = __builtin_bit_cast(bf16x8, fp4_words(u[e], f));
 #pragma unroll
-          for (int p = NQ - 1; p >= 0; --p) x[hh] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[p][s], x[hh], 0, 0, 0);
+          for (int y = NQ - 1; y >= 0; --y)
+            x[hh] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[y][blk + e], x[hh], 0, 0, 0);
         }
+      }
     }
 #pragma unroll
     for (int hh = 0; hh < H; ++hh) settle(x[hh]);
-#pragma unroll
-    for (int hh = 0; hh < H; ++hh)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) x[hh][r] *= scale;
     uint32_t gone = 0;   // keys of this lane's eight that the query does not see
     if (!whole) {
 #pragma unroll
       for (int hh = 0; hh < H; ++hh)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const int s = y.slot0 + 16 * hh + 4 * g + r;
-          const bool see = y.ok[hh] && s < len && (!a.window || len - 1 - s < a.window || s < a.sinks);
+          const int s = s0 + 16 * hh + 4 * g + r;
+          const bool see = ((ok >> hh) & 1u) && s < len && (!a.window || len - 1 - s < a.window || s < a.sinks);
           if (!see) {
             x[hh][r] = -INFINITY;
             gone |= 1u << (4 * hh + r);
@@ -201,55 +285,90 @@ decode4_kernel(CacheView c, CacheScales sc4, AttendArgs a, DecodeScratch sc, int
       for (int r = 0; r < 4; ++r) mt = fmaxf(mt, x[hh][r]);
     mt = fmaxf(mt, xor_lane<16>(mt));
     mt = fmaxf(mt, xor_lane<32>(mt));
-    const float mn = fmaxf(m, mt), base = mn == -INFINITY ? 0.f : mn;
-    const float f = __builtin_amdgcn_exp2f(m - base);
-    m = mn;
-    float sum = 0.f;
+    // the running maximum follows in steps of at least 8 (base 2): weights stay
+    // below 2^8 and most tiles rescale nothing
+    if (__any(mt > m + slack)) {
+      const float mn = mt > m + slack ? mt : m;
+      const float f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - mn) * cs);
+      m = mn;
+      l *= f;
+#pragma unroll
+      for (int n = 0; n < NO; ++n) o[n] *= f;
+    }
+    const float base = m == -INFINITY ? 0.f : m * cs;
     bf16x8 p[NP];
 #pragma unroll
     for (int hh = 0; hh < H; ++hh)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const float e = __builtin_amdgcn_exp2f(x[hh][r] - base);
-        sum += e;
+        const float e = __builtin_amdgcn_exp2f(fmaf(x[hh][r], cs, -base));
+        l += e;   // this lane group's keys; joined at the end
         const int at = 4 * hh + r;
+        // (no part of a weight above zero is zero: an infinite value, which scales
+        // from 2^126 on have, stays what it is)
+        const uint32_t u = __float_as_uint(e) & 0xFFFF0000u;
+        const float rest = e - __uint_as_float(u);
+        p[0][at] = __builtin_bit_cast(__bf16, static_cast<uint16_t>(u >> 16));
         if constexpr (NP == 2) {
-          const uint32_t u = __float_as_uint(e) & 0xFFFF0000u;
-          p[0][at] = __builtin_bit_cast(__bf16, static_cast<uint16_t>(u >> 16));
-          // (no part of a weight above zero is zero: an infinite value, which
-          // scales from 2^126 on have, stays what it is)
-          p[1][at] = static_cast<__bf16>(fmaxf(e - __uint_as_float(u), e * 0x1p-24f));
+          p[1][at] = static_cast<__bf16>(fmaxf(rest, e * 0x1p-24f));
         } else {
-          const uint32_t u = __float_as_uint(e) & 0xFFFF0000u;
-          const float rest = e - __uint_as_float(u);
           const uint32_t v = __float_as_uint(fmaxf(rest, e * 0x1p-25f)) & 0xFFFF0000u;
-          p[0][at] = __builtin_bit_cast(__bf16, static_cast<uint16_t>(u >> 16));
           p[1][at] = __builtin_bit_cast(__bf16, static_cast<uint16_t>(v >> 16));
           p[2][at] = static_cast<__bf16>(fmaxf(rest - __uint_as_float(v), e * 0x1p-33f));
         }
       }
-    l = l * f + sum;   // this lane group's keys; joined at the end
+    uint32_t sv[H][SB];
 #pragma unroll
-    for (int n = 0; n < NO; ++n) o[n] *= f;
+    for (int hh = 0; hh < H; ++hh) {
+      const shared_u8* ps = in + L::scales_at(true, hh, 4 * g);
+      if constexpr (SB == 1) sv[hh][0] = ld_shared<uint32_t>(ps);
+      if constexpr (SB == 2) { const u32x2 y = ld_shared<u32x2>(ps); sv[hh][0] = y.x; sv[hh][1] = y.y; }
+      if constexpr (SB >= 4) {
+#pragma unroll
+        for (int e = 0; e < SB / 4; ++e) {
+          const u32x4 y = ld_shared<u32x4>(ps + 16 * e);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) sv[hh][4 * e + k] = y[k];
+        }
+      }
+    }
 #pragma unroll
     for (int n = 0; n < R::count; ++n) {
-      const int pairs = R::size(n) / 32, blk = R::base(n) / 32;   // pairs of elements a lane has of each key
-      uint32_t v[H][4][4];
+      const int size = R::size(n), pairs = size / 32, blk = R::base(n) / 32;   // pairs of elements a lane has of each key
+      const int mine = size == 128 ? i16 >> 2 : size == 64 ? i16 >> 3 : 0;
+      uint32_t codes[H][4], v[H][4][4];
 #pragma unroll
       for (int hh = 0; hh < H; ++hh)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const int sh = R::size(n) == 128 ? 8 * (i16 >> 2) : R::size(n) == 64 ? 8 * (i16 >> 3) : 0;
+          const shared_u8* p4 = in + L::v_at(hh, 4 * g + r, blk + mine);
+          codes[hh][r] = size == 128  ? ld_shared<uint32_t>(p4 + 4 * (i16 & 3))
+                         : size == 64 ? ld_shared<uint16_t>(p4 + 2 * (i16 & 7))
+                                      : p4[i16];
+        }
+      uint32_t es[H][4];
+#pragma unroll
+      for (int hh = 0; hh < H; ++hh)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
           const int at = r * SB + blk;
-          uint32_t e = (y.sv[hh][at / 4] >> (8 * (at % 4) + sh)) & 255u, codes = y.v[hh][r][n];
-          if (!whole && (gone >> (4 * hh + r)) & 1u) {   // a weight of zero does not silence a NaN
-            e = 0u;
-            codes = 0u;
-          }
-          const float fs = scale_of(e);
-          v[hh][r][0] = fp4_pair<0>(codes, fs);
-          if (pairs > 1) v[hh][r][1] = fp4_pair<1>(codes, fs);
-          if (pairs > 2) { v[hh][r][2] = fp4_pair<2>(codes, fs); v[hh][r][3] = fp4_pair<3>(codes, fs); }
+          es[hh][r] = scale_at_bits(sv[hh][at / 4], at % 4 + mine);
+        }
+      if (!whole) {   // a weight of zero does not silence a NaN
+#pragma unroll
+        for (int hh = 0; hh < H; ++hh)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if ((gone >> (4 * hh + r)) & 1u) codes[hh][r] = es[hh][r] = 0u;
+      }
+#pragma unroll
+      for (int hh = 0; hh < H; ++hh)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float fs = __uint_as_float(es[hh][r]);
+          v[hh][r][0] = fp4_pair<0>(codes[hh][r], fs);
+          if (pairs > 1) v[hh][r][1] = fp4_pair<1>(codes[hh][r], fs);
+          if (pairs > 2) { v[hh][r][2] = fp4_pair<2>(codes[hh][r], fs); v[hh][r][3] = fp4_pair<3>(codes[hh][r], fs); }
         }
 #pragma unroll
       for (int j = 0; j < 2 * pairs; ++j) {
@@ -269,18 +388,52 @@ decode4_kernel(CacheView c, CacheScales sc4, AttendArgs a, DecodeScratch sc, int
     }
   };
 
-  Tile even, odd;
-  int tile = t0 + w;
-  if (tile < t1) load(tile, even);
-  for (; tile < t1; tile += 2 * WAVES) {
-    if (tile + WAVES < t1) load(tile + WAVES, odd);
-    compute(even);
-    if (tile + WAVES >= t1) break;
-    if (tile + 2 * WAVES < t1) load(tile + 2 * WAVES, even);
-    compute(odd);
+  // Page ids come one tile before their loads.
+  shared_u8* const at0 = (shared_u8*)ring0 + w * L::kBytes;
+  shared_u8* const at1 = (shared_u8*)ring1 + w * L::kBytes;
+  shared_u8* const at2 = kTiles > 2 ? (shared_u8*)ring2 + w * L::kBytes : at0;
+  unsigned ok0 = 0, ok1 = 0, ok2 = 0;
+  int tile = t0 + w, id[H];
+  auto next = [&](int t, unsigned* ok, shared_u8* to) __attribute__((always_inline)) {
+    if (t >= t1) return;
+    *ok = on_pages(t, id);
+    issue(t, id, *ok, to);
+    ids_of(t + WAVES, id);
+  };
+  // the tile t while those behind it are on their way
+  auto step = [&](int t, unsigned ok, const shared_u8* in) __attribute__((always_inline)) {
+    if (kTiles > 2 && t + 2 * WAVES < t1) arrive<2 * L::kInFlight>();
+    else if (t + WAVES < t1) arrive<L::kInFlight>();
+    else arrive<0>();
+    compute(t, ok, in);
+  };
+  if (tile < t1) {
+    ids_of(tile, id);
+    next(tile, &ok0, at0);
+    if constexpr (kTiles > 2) next(tile + WAVES, &ok1, at1);
+  }
+  for (; tile < t1; tile += kTiles * WAVES) {
+    if constexpr (kTiles > 2) {
+      next(tile + 2 * WAVES, &ok2, at2);
+      step(tile, ok0, at0);
+      if (tile + WAVES >= t1) break;
+      next(tile + 3 * WAVES, &ok0, at0);
+      step(tile + WAVES, ok1, at1);
+      if (tile + 2 * WAVES >= t1) break;
+      next(tile + 4 * WAVES, &ok1, at1);
+      step(tile + 2 * WAVES, ok2, at2);
+    } else {
+      next(tile + WAVES, &ok1, at1);
+      step(tile, ok0, at0);
+      if (tile + WAVES >= t1) break;
+      next(tile + 2 * WAVES, &ok0, at0);
+      step(tile + WAVES, ok1, at1);
+    }
   }
   asm volatile("s_nop 15\n\ts_nop 7" ::: "memory");   // (see settle)
   __builtin_amdgcn_sched_barrier(0);
+  m = m * cs;          // (as the parts' maxima are joined)
+  float(*const red)[16 * DH] = reinterpret_cast<float(*)[16 * DH]>(ring0);
 
   // the waves' parts on their common maximum, added in a fixed order
   l = add_xor32(add_xor16(l));
@@ -342,9 +495,15 @@ decode4_kernel(CacheView c, CacheScales sc4, AttendArgs a, DecodeScratch sc, int
 
 static int decode4_qtiles(const CacheView& c) { return (c.hg + 15) / 16; }
 
+// As many blocks as find room on the chip together, three to a CU (us with 512, 768,
+// 1024 and 1536: 8 requests of 100000 to 131072 slots, 32 heads on 8 of 128, 205, 200, 197 and
+// 194; 64 of 200 to 4096, 28 on 4, 28.2, 26.3, 27.5 and 28; 16 of them 13.0, 13.8, 15.4
+// and 17).  Splits of one length for all sequences, so that short ones have fewer, were
+// slower: 210 and 28.1.
+constexpr int kDecode4Blocks = 768;
 static int decode4_splits(const CacheView& c, int qtiles) {
   const long long groups = static_cast<long long>(c.n_seq) * c.hkv * qtiles;
-  return used_splits((c.cap + kTile4 - 1) / kTile4, static_cast<int>((1024 + groups - 1) / groups));
+  return used_splits((c.cap + kTile4 - 1) / kTile4, static_cast<int>((kDecode4Blocks + groups - 1) / groups));
 }
 
 // One block a head and no second kernel, as over pages of bf16.
