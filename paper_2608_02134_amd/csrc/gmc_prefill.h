@@ -442,53 +442,68 @@ __device__ __forceinline__ void prefill_block(const CacheView& c, const CacheSca
     __syncthreads();
   };
 
-  // Pages of 4 bits: a thread has kUnits blocks of 32 values of a tile, K and V after
-  // each other, in registers while the tile before is computed.
-  constexpr int BR = DH / 32, kHalf = KT * BR, kUnits = (2 * kHalf + 64 * kPreWaves - 1) / (64 * kPreWaves);
-  u32x4 codes[Q4 ? kUnits : 1];
+  // Pages of 4 bits: a run of 16 slots has 32 BR blocks of 32 values, K's and then
+  // V's; a wave takes 64 of them at a time, of one run, and kUnits times in a tile.
+  // Their codes go into shared memory, from where the same lane takes them a tile
+  // later (in registers they were what spilt).
+  constexpr int BR = DH / 32, kOfRun = (BR + 1) / 2, kUnits = (GROUPS * kOfRun + kPreWaves - 1) / kPreWaves;
+  __shared__ __align__(16) unsigned char code_blocks[Q4 ? kUnits * kPreWaves * 1024 : 16];
+  shared_u8* const my_codes = (shared_u8*)code_blocks + 1024 * w;
   uint32_t scales[Q4 ? kUnits : 1];
-  // Block x: of V or K, its row and which of the row's.  Neighbouring rows of a
-  // run lie four lanes' blocks apart, as the rows r, r + 4, r + 8 and r + 12
-  // have their chunks on different banks.
-  auto unit = [&](int u, bool* value, int* r, int* blk) GMC_INLINE {
-    const int x = u * 64 * kPreWaves + static_cast<int>(threadIdx.x), y = x >= kHalf ? x - kHalf : x;
-    const int at = y / BR;
-    *value = x >= kHalf;
+  // The run of the wave's unit u, and of its lane: whether it has a block (of V or
+  // K), the block's row in the run and which of the row's it is.  Rows follow each
+  // other by fours, as the chunks of r, r + 4, r + 8 and r + 12 stand on different
+  // banks.
+  auto run_of = [&](int u) GMC_INLINE { return (w + kPreWaves * u) / kOfRun; };
+  auto block_of = [&](int u, bool* value, int* r, int* blk) GMC_INLINE {
+    const int x = 64 * ((w + kPreWaves * u) % kOfRun) + lane, y = x >= 16 * BR ? x - 16 * BR : x, at = y / BR;
+    *value = x >= 16 * BR;
     *blk = y - at * BR;
-    *r = (at & ~15) | ((at & 3) << 2) | ((at >> 2) & 3);
-    return x < 2 * kHalf;
+    *r = ((at & 3) << 2) | ((at >> 2) & 3);
+    return x < 32 * BR;
   };
   auto fetch4 = [&](int it, int ids) GMC_INLINE -> unsigned {
     const unsigned ok = on_pages(it, ids);
-    const int s0 = slot0(it);
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
+      const int run = run_of(u);
+      if (run >= GROUPS) break;
       bool value;
       int r, blk;
-      const bool some = unit(u, &value, &r, &blk);
-      const int id = __shfl(ids, (r >> 4) & (GROUPS - 1)), s = s0 + r;
-      codes[u] = u32x4{0u, 0u, 0u, 0u};
-      scales[u] = 0u;
-      if (some && s < wk.len && ((ok >> (r >> 4)) & 1u)) {
-        const long long at = ((static_cast<long long>(id) * c.hkv + h) << c.shift) + (s & (c.page - 1));
-        codes[u] = *reinterpret_cast<const u32x4*>(static_cast<const char*>(value ? c.v : c.k) + at * (DH / 2) + 16 * blk);
-        scales[u] = (value ? s4.v : s4.k)[at * scale_bytes(DH) + blk];
+      const bool some = block_of(u, &value, &r, &blk);
+      const int s = slot0(it) + 16 * run, held = (ok >> run) & 1u ? wk.len - s : 0;   // rows of the run that are held
+      const long long row =
+          held > 0 ? ((static_cast<long long>(__builtin_amdgcn_readlane(ids, run)) * c.hkv + h) << c.shift) + (s & (c.page - 1)) : 0;
+      const char* from = static_cast<const char*>(value ? c.v : c.k) + row * (DH / 2) + (r * (DH / 2) + 16 * blk);
+      const uint8_t* scale = (value ? s4.v : s4.k) + row * scale_bytes(DH) + (r * scale_bytes(DH) + blk);
+      if (held >= 16 && 32 * BR % 64 == 0) {
+        scales[u] = *scale;
+      } else {
+        scales[u] = 0u;
+        if (some && r < held) scales[u] = *scale;
+        else from = reinterpret_cast<const char*>(kZeroRow);
       }
+      __builtin_amdgcn_global_load_lds((const global_u32*)from, my_codes + 1024 * kPreWaves * u, 16, 0, 0);
     }
     return ok;
   };
   auto spread4 = [&](shared_u8* ks, shared_u8* vs) GMC_INLINE {
+    __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
+    asm volatile("" ::: "memory");
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
+      const int run = run_of(u);
+      if (run >= GROUPS) break;
       bool value;
       int r, blk;
-      if (!unit(u, &value, &r, &blk)) break;
-      shared_u8* const to = (value ? vs : ks) + r * PITCH;
+      if (!block_of(u, &value, &r, &blk)) break;
+      shared_u8* const to = (value ? vs : ks) + (16 * run + r) * PITCH;
       const float f = scale_of(scales[u]);
+      const u32x4 codes = ld_shared<u32x4>(my_codes + 1024 * kPreWaves * u + 16 * lane);
       typedef __attribute__((address_space(3))) u32x4 shared_u32x4;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const uint4 y = fp4_words(codes[u][e], f);
+        const uint4 y = fp4_words(codes[e], f);
         if constexpr (sizeof(T) == 2) {
           *reinterpret_cast<shared_u32x4*>(to + 16 * KTile::place(r, 4 * blk + e)) = u32x4{y.x, y.y, y.z, y.w};
         } else {
@@ -499,6 +514,7 @@ __device__ __forceinline__ void prefill_block(const CacheView& c, const CacheSca
         }
       }
     }
+    __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0): the codes have been read before the next ones come
   };
 
   shared_u8* const kb0 = (shared_u8*)k_even;

@@ -397,6 +397,7 @@ decode4_kernel(CacheView c, CacheScales sc4, AttendArgs a, DecodeScratch sc, int
   auto next = [&](int t, unsigned* ok, shared_u8* to) __attribute__((always_inline)) {
     if (t >= t1) return;
     *ok = on_pages(t, id);
+    __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0): what was read of the tile before is in registers
     issue(t, id, *ok, to);
     ids_of(t + WAVES, id);
   };
