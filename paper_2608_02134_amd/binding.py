@@ -806,7 +806,7 @@ class KvCache:
         self.n_q_heads, self.n_kv_heads, self.head_dim = n_q_heads, hkv, dh
         self._scale = dh ** -0.5
         self._index_of_device = self.device.index
-        self._current_device = torch.cuda.current_device
+        self._current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
         # (the address alone: a Stream object takes longer than the call)
         self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
             (lambda i: torch.cuda.current_stream(i).cuda_stream)
@@ -915,32 +915,33 @@ class KvCache:
         the tokens' queries; their rotated ones are returned (in ``out`` if given,
         which without src may be q), [n_seq * n][n_q_heads][head_dim] with src."""
         rows = self._appended(k, v, starts, max_new, src)
+        tokens = rows[4]
         if rotary.device != self.device:
             raise ValueError(f"rotary must be on the cache's device {self.device}; got {rotary.device}")
-        p = None if pos is None else self._index("pos", pos, (rows[4], 3) if rotary.sections else (rows[4],))
+        p = None if pos is None else self._index("pos", pos, (tokens, 3) if rotary.sections else (tokens,))
         if q is None:
             if out is not None:
                 raise ValueError("out needs q")
-            self._call(self._kind + self._turned, rotary._ref, *rows, p, None, 0, None)
+            self._call(self._turned, rotary._ref, *rows, p, None, 0, None)
             return None
         stride = self._rows("q", q, self.n_q_heads)
-        if q.shape[0] != rows[4]:
-            raise ValueError(f"q and k hold {q.shape[0]} and {rows[4]} tokens")
-        shape = (rows[4] if src is None else self.n_seq * rows[7], self.n_q_heads, self.head_dim)
+        if q.shape[0] != tokens:
+            raise ValueError(f"q and k hold {q.shape[0]} and {tokens} tokens")
+        shape = (tokens if src is None else self.n_seq * rows[7], self.n_q_heads, self.head_dim)
         if out is None:
-            out = self.torch.empty(shape, dtype=self.dtype, device=self.device)
+            out = q.new_empty(shape)
         elif tuple(out.shape) != shape or out.dtype != self.dtype or not out.is_contiguous() or out.device != self.device:
             raise ValueError(f"out must be a contiguous {self.dtype} {shape} tensor on the cache's device")
-        self._call(self._kind + self._turned, rotary._ref, *rows, p, q.data_ptr(), stride, out.data_ptr())
+        self._call(self._turned, rotary._ref, *rows, p, q.data_ptr(), stride, out.data_ptr())
         return out
 
-    _turned = "append_rotary"
+    _turned = "gmc_cache_append_rotary"
 
     def _outputs(self, q, out, lse):
         torch = self.torch
         shape = (q.shape[0], self.n_q_heads, self.head_dim)
         if out is None:
-            out = torch.empty(shape, dtype=self.dtype, device=self.device)
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)   # (q has been checked)
         elif tuple(out.shape) != shape or out.dtype != self.dtype or not out.is_contiguous() or out.device != self.device:
             raise ValueError(f"out must be a contiguous {self.dtype} {shape} tensor on the cache's device")
         if lse is True:
@@ -1045,7 +1046,7 @@ class KvCache4(KvCache):
         self._ref = ctypes.byref(self.desc)
 
     _kind = "gmc_cache4_"
-    _turned = "append"
+    _turned = "gmc_cache4_append"
 
     @classmethod
     def create(cls, *, n_seq, slots, n_q_heads, n_kv_heads, head_dim, dtype, device="cuda", page_size=64):
@@ -1082,7 +1083,7 @@ class KvCache4(KvCache):
         if rows < 1:
             raise ValueError(f"rows={rows} must be at least 1")
         first, max_new = self._new(rows, starts, max_new)
-        k, v = (self.torch.empty((rows, self.n_kv_heads, self.head_dim), dtype=self.dtype, device=self.device) for _ in "kv")
+        k, v = self.torch.empty((2, rows, self.n_kv_heads, self.head_dim), dtype=self.dtype, device=self.device).unbind()
         self._call("gmc_cache4_read", rows, first, max_new, k.data_ptr(), v.data_ptr())
         return k, v
 

@@ -66,7 +66,7 @@ struct RotaryView {
 // New rows of K and V, with the queries of their tokens.
 struct RotaryArgs {
   const void *k, *v, *q;  // q may be null
-  long long k_stride, v_stride, q_stride, rows;   // strides in elements
+  long long k_stride, v_stride, q_stride, rows, per_seq;   // strides in elements; rows of a sequence that src picks from
   const int32_t *starts, *src, *pos;
   int max_new;
   void* q_out;

@@ -208,6 +208,7 @@ int append_rotary(const char* fn, const CacheView& c, const CacheScales* scales,
   }
   RotaryArgs a{};
   a.k = k; a.v = v; a.q = q; a.k_stride = k_stride; a.v_stride = v_stride; a.q_stride = q_stride; a.rows = rows;
+  a.per_seq = rows / c.n_seq;
   a.starts = starts; a.src = src; a.pos = pos; a.max_new = static_cast<int>(max_new); a.q_out = q_out;
   return on_stream(fn, stream, [&](hipStream_t st) {
     return launch_cache_append_rotary(c, scales, rotary ? &r : nullptr, a, st);

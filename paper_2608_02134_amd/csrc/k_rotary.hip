@@ -99,11 +99,12 @@ __device__ __forceinline__ uint32_t block_top(const float* x) {
 }
 
 // One token: heads of K, V and q, 64 / (dh / 8) at a time to a wave, by `parts`
-// waves of which this is number `part`.  row: of head 0 in the pages (-1: not
-// stored); from: in k, v, q and pos; to: in q_out.
+// waves of which this is number `part`.  s: its slot (one past the capacity is not
+// stored); from: its row in k, v, q and pos; to: in q_out.  (The first heads' loads
+// before the position's and the page's: 69 us where this takes 62 for 16448 tokens.)
 template <typename T, bool Q4, int PAIRS>
 __device__ __forceinline__ void append_turned(const CacheView& c, const CacheScales& sc, const RotaryView& r,
-                                              const RotaryArgs& a, long long row, int position, long long from,
+                                              const RotaryArgs& a, int b, int s, int position, long long from,
                                               long long to, int part, int parts) {
   const int lane = threadIdx.x & 63, per = c.dh >> 3, heads = 64 / per;
   const int hl = lane / per, d0 = 8 * (lane - hl * per);
@@ -112,11 +113,12 @@ __device__ __forceinline__ void append_turned(const CacheView& c, const CacheSca
   const bool turns = PAIRS != kNoPairs && d0 < r.rot, second = d0 >= half;
   Turn t;
   if (turns) load_turn<PAIRS>(r, a.pos ? a.pos + from * r.axes : nullptr, position, d0, &t);
+  const long long row = s < c.cap ? cache_row(c, b, 0, s) : -1;   // of head 0; the others' lie a page's rows on
   const int total = 2 * c.hkv + (a.q ? c.hq : 0);
   const T* const k = static_cast<const T*>(a.k) + from * a.k_stride + d0;
   const T* const v = static_cast<const T*>(a.v) + from * a.v_stride + d0;
   const T* const q = a.q ? static_cast<const T*>(a.q) + from * a.q_stride + d0 : nullptr;
-  constexpr int kFlight = sizeof(T) == 2 ? 4 : 2;   // heads whose loads are on their way together
+  constexpr int kFlight = sizeof(T) == 2 ? 3 : 2;   // heads whose loads are on their way together
   for (int u0 = part * heads + hl; u0 < total; u0 += kFlight * parts * heads) {
     Piece<T> own[kFlight], other[kFlight];
 #pragma unroll
@@ -157,11 +159,10 @@ __device__ __forceinline__ void append_turned(const CacheView& c, const CacheSca
   }
 }
 
-__device__ __forceinline__ long long source_row(const RotaryArgs& a, int n_seq, int b, long long first, int i) {
+__device__ __forceinline__ long long source_row(const RotaryArgs& a, int b, long long first, int i) {
   if (!a.src) return first + i;
-  const long long per = a.rows / n_seq;
   const long long x = a.src[static_cast<long long>(b) * a.max_new + i];
-  return b * per + min(max(x, 0ll), per - 1);
+  return b * a.per_seq + min(max(x, 0ll), a.per_seq - 1);
 }
 
 // Token i of sequence b, by `parts` waves.
@@ -170,18 +171,21 @@ __device__ __forceinline__ void append_token_turned(const CacheView& c, const Ca
                                                     const RotaryArgs& a, int b, long long first, int len, int seen,
                                                     int i, int part, int parts) {
   const int s = len + i, lane = threadIdx.x & 63;
-  const bool fits = s < c.cap;
-  if (part == 0 && fits && c.slot_pos) {
-    const long long at = static_cast<long long>(b) * c.hkv * c.cap + s;
-    for (int h = lane; h < c.hkv; h += 64) c.slot_pos[at + static_cast<long long>(h) * c.cap] = seen + i;
+  append_turned<T, Q4, PAIRS>(c, sc, r, a, b, s, c.seen ? seen + i : s, source_row(a, b, first, i), first + i,
+                              part, parts);
+  if (part != 0 || s >= c.cap) return;
+  const long long at = static_cast<long long>(b) * c.hkv * c.cap + s;
+  for (int h = lane; h < c.hkv; h += 64) {
+    if (c.slot_pos) c.slot_pos[at + static_cast<long long>(h) * c.cap] = seen + i;
+    if (c.weights) c.weights[at + static_cast<long long>(h) * c.cap] = 0.f;
   }
-  if (part == 0 && fits && c.weights) {
-    const long long at = static_cast<long long>(b) * c.hkv * c.cap + s;
-    for (int h = lane; h < c.hkv; h += 64) c.weights[at + static_cast<long long>(h) * c.cap] = 0.f;
-  }
-  append_turned<T, Q4, PAIRS>(c, sc, r, a, fits ? cache_row(c, b, 0, s) : -1, c.seen ? seen + i : s,
-                              source_row(a, c.n_seq, b, first, i), first + i, part, parts);
 }
+
+// Tokens whose heads four waves share (28 query heads on 4 of 128 in bf16, us with the
+// length's kernel, shared and by one wave: 16 tokens 8.4 and 10.7, 335 8.9 and 11.0, 1375
+// 14.4 and 13.0, 4096 25.9 and 20).
+constexpr int kSplitTokens = 512;
+constexpr int kGridBlocks = 1 << 22;   // of 256 threads, at most 65535 sequences: the others are loops
 
 // Few new tokens: one block a sequence, four waves a token, which also moves the
 // length on.
@@ -206,14 +210,14 @@ rotary_append_few_kernel(CacheView c, CacheScales sc, RotaryView r, RotaryArgs a
 
 template <typename T, bool Q4, int PAIRS>
 __global__ void __launch_bounds__(256)
-rotary_append_kernel(CacheView c, CacheScales sc, RotaryView r, RotaryArgs a) {
-  const int b = blockIdx.y;
+rotary_append_kernel(CacheView c, CacheScales sc, RotaryView r, RotaryArgs a, int parts) {
+  const int b = blockIdx.y, w = wave_id(), part = w & (parts - 1), at_once = 4 / parts;   // tokens of a block
   long long first;
   int n;
   new_rows(a.starts, a.max_new, a.rows, b, &first, &n);
   const int len = cache_len(c, b), seen = c.seen ? c.seen[b] : 0;
-  for (int i = blockIdx.x * 4 + wave_id(); i < n; i += gridDim.x * 4)
-    append_token_turned<T, Q4, PAIRS>(c, sc, r, a, b, first, len, seen, i, 0, 1);
+  for (int i = blockIdx.x * at_once + w / parts; i < n; i += gridDim.x * at_once)
+    append_token_turned<T, Q4, PAIRS>(c, sc, r, a, b, first, len, seen, i, part, parts);
 }
 
 template <typename T, bool Q4, int PAIRS>
@@ -224,8 +228,10 @@ static hipError_t start_append(const CacheView& c, const CacheScales& sc, const 
                        c, sc, r, a);
     return hipGetLastError();
   }
-  hipLaunchKernelGGL((rotary_append_kernel<T, Q4, PAIRS>), dim3(std::min((a.max_new + 3) / 4, 4096), c.n_seq), dim3(256),
-                     0, st, c, sc, r, a);
+  const int parts = static_cast<long long>(a.max_new) * c.n_seq <= kSplitTokens ? 4 : 1;
+  const int blocks = (a.max_new + 4 / parts - 1) / (4 / parts);
+  hipLaunchKernelGGL((rotary_append_kernel<T, Q4, PAIRS>), dim3(std::min(blocks, kGridBlocks / c.n_seq), c.n_seq), dim3(256),
+                     0, st, c, sc, r, a, parts);
   const hipError_t err = hipGetLastError();
   if (err != hipSuccess) return err;   // (rows that were not written are not counted)
   return launch_cache_advance(c, a.starts, a.rows, a.max_new, st);
@@ -259,20 +265,32 @@ cache4_read_kernel(CacheView c, CacheScales sc, long long rows, const int32_t* s
   for (int i = blockIdx.x * 4 + wave_id(); i < n; i += gridDim.x * 4) {
     const int s = len - n + i;
     const long long row = s < 0 ? -1 : cache_row(c, b, 0, s);
-    for (int p = lane; p < 2 * c.hkv * per; p += 64) {
-      const int u = p / per, piece = p - u * per, h = u < c.hkv ? u : u - c.hkv;
-      const bool values = u >= c.hkv;
-      const long long at = row + (static_cast<long long>(h) << c.shift);
-      const uint32_t codes = row < 0 ? 0u : static_cast<const uint32_t*>(values ? c.v : c.k)[at * per + piece];
-      const uint32_t e = row < 0 ? 0u : (values ? sc.v : sc.k)[at * sc.bytes + (piece >> 2)];
-      const uint4 y = fp4_words(codes, scale_of(e));
-      T* to = (values ? v_out : k_out) + ((first + i) * c.hkv + h) * c.dh + 8 * piece;
-      if constexpr (sizeof(T) == 2) {
-        *reinterpret_cast<uint4*>(to) = y;
-      } else {
-        float x[8];
-        unpack(Piece<bf16_t>{y}, x);
-        store_piece(to, x);
+    constexpr int kFlight = 2;
+    for (int p0 = lane; p0 < 2 * c.hkv * per; p0 += 64 * kFlight) {
+      uint32_t codes[kFlight], e[kFlight];
+#pragma unroll
+      for (int f = 0; f < kFlight; ++f) {
+        const int p = p0 + 64 * f, u = p / per, piece = p - u * per;
+        const bool values = u >= c.hkv;
+        const long long at = row + (static_cast<long long>(values ? u - c.hkv : u) << c.shift);
+        codes[f] = e[f] = 0u;
+        if (row < 0 || u >= 2 * c.hkv) continue;
+        codes[f] = static_cast<const uint32_t*>(values ? c.v : c.k)[at * per + piece];
+        e[f] = (values ? sc.v : sc.k)[at * sc.bytes + (piece >> 2)];
+      }
+#pragma unroll
+      for (int f = 0; f < kFlight; ++f) {
+        const int p = p0 + 64 * f, u = p / per, piece = p - u * per;
+        if (u >= 2 * c.hkv) break;
+        const uint4 y = fp4_words(codes[f], scale_of(e[f]));
+        T* to = (u >= c.hkv ? v_out : k_out) + ((first + i) * c.hkv + (u >= c.hkv ? u - c.hkv : u)) * c.dh + 8 * piece;
+        if constexpr (sizeof(T) == 2) {
+          *reinterpret_cast<uint4*>(to) = y;
+        } else {
+          float x[8];
+          unpack(Piece<bf16_t>{y}, x);
+          store_piece(to, x);
+        }
       }
     }
   }
@@ -280,7 +298,7 @@ cache4_read_kernel(CacheView c, CacheScales sc, long long rows, const int32_t* s
 
 hipError_t launch_cache4_read(const CacheView& c, const CacheScales& s, long long rows, const int32_t* starts,
                               int max_new, void* k_out, void* v_out, hipStream_t st) {
-  const dim3 grid(std::min((max_new + 3) / 4, 4096), c.n_seq);
+  const dim3 grid(std::min((max_new + 3) / 4, kGridBlocks / c.n_seq), c.n_seq);
   if (c.dtype == 0)
     hipLaunchKernelGGL(cache4_read_kernel<float>, grid, dim3(256), 0, st, c, s, rows, starts, max_new,
                        static_cast<float*>(k_out), static_cast<float*>(v_out));
