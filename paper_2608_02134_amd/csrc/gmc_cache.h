@@ -128,7 +128,7 @@ hipError_t launch_cache_append(const CacheView& c, const void* k, const void* v,
 
 // Attention of every query row over its sequence's cache.  scratch:
 // prefill_scratch_bytes of any content.
-long long prefill_scratch_bytes(const CacheView& c, int max_new);
+long long prefill_scratch_bytes(const CacheView& c, int max_new, bool four_bits = false);
 hipError_t launch_cache_prefill(const CacheView& c, const AttendArgs& a, void* scratch, hipStream_t st);
 
 // The same for one query row per sequence (a.starts null, a.max_new 1), with

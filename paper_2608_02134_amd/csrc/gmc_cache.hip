@@ -219,8 +219,8 @@ int64_t round256(int64_t x) { return (x + 255) / 256 * 256; }
 
 int64_t decode_bytes(const CacheView& c, bool accumulate) { return round256(decode_scratch_bytes(c, accumulate)); }
 int64_t decode4_bytes(const CacheView& c) { return round256(decode4_scratch_bytes(c)); }
-int64_t prefill_bytes(const CacheView& c, int64_t max_new) {
-  return round256(prefill_scratch_bytes(c, static_cast<int>(max_new)));
+int64_t prefill_bytes(const CacheView& c, int64_t max_new, bool four_bits = false) {
+  return round256(prefill_scratch_bytes(c, static_cast<int>(max_new), four_bits));
 }
 int64_t evict_bytes(const CacheView& c) { return round256(evict_scratch_bytes(c)); }
 
@@ -367,7 +367,7 @@ int64_t gmc_cache4_prefill_bytes(const gmc_cache4* cache, int64_t max_new) {
   if (rc != GMC_OK) return rc;
   if (max_new < 1 || max_new > c.cap)
     return set_error(GMC_ERR_ARG, "%s: max_new=%lld out of [1, %d]", fn, ll(max_new), c.cap);
-  return prefill_bytes(c, max_new);
+  return prefill_bytes(c, max_new, true);
 }
 
 int gmc_cache4_prefill(const gmc_cache4* cache, const void* q, int64_t q_stride, int64_t rows, const int32_t* starts,
@@ -381,7 +381,7 @@ int gmc_cache4_prefill(const gmc_cache4* cache, const void* q, int64_t q_stride,
   if ((rc = check_attend(fn, c, q, q_stride, scale, window, sinks, out)) != GMC_OK) return rc;
   if ((rc = check_new(fn, c, starts, max_new, rows)) != GMC_OK) return rc;
   if ((rc = check_blocks(fn, c, max_new)) != GMC_OK) return rc;
-  if ((rc = check_workspace(fn, workspace, workspace_bytes, prefill_bytes(c, max_new))) != GMC_OK) return rc;
+  if ((rc = check_workspace(fn, workspace, workspace_bytes, prefill_bytes(c, max_new, true))) != GMC_OK) return rc;
   const AttendArgs a = attend_args(q, q_stride, rows, starts, max_new, scale, window, sinks, out, lse);
   return on_stream(fn, stream, [&](hipStream_t st) { return launch_cache4_prefill(c, s, a, workspace, st); });
 }

@@ -123,7 +123,10 @@ static int pre_row_blocks(const CacheView& c, int max_new) {
 // with 16, 26.2 with 10, 29.8 with 25; 10 over 2000 14.1 with 15, 19.6 with 5;
 // 200 over 500 (12 on 12 of 96, 2 sequences) 15.1 with 1, 16.7 with 4; fp32 (8 on
 // 2 of 64) 300 tokens 17.0 with 5, 26.6 with 2.
-static int pre_splits(const CacheView& c, int max_new) {
+// Over 4 bits also what a tile costs where two blocks share a CU (77 tokens over
+// 4100 slots 29.8 us with 240 blocks, 32.4 with 280; three such requests 43.7 with 480, 57
+// with 240; 16 over 32768 35.6 with 256, 38.6 with 348).
+static int pre_splits(const CacheView& c, int max_new, bool four_bits) {
   const int kt = pre_key_tile(c), tiles = (c.cap + kt - 1) / kt;
   const long long blocks = static_cast<long long>(pre_row_blocks(c, max_new)) * c.hkv * c.n_seq;
   const double tile = (c.dtype == 0 ? 1.9 / (32 * 64) : 1.7 / (64 * 128)) * kt * c.dh;
@@ -131,7 +134,8 @@ static int pre_splits(const CacheView& c, int max_new) {
   int best = 1;
   double least = tile * tiles;
   for (int s = 2; s <= tiles / 2 && blocks * s <= 512; ++s) {
-    const double time = tile * tiles / s + 4 + part * s;
+    const double shared = four_bits && blocks * s > 256 ? 1.5 : 1;
+    const double time = shared * tile * tiles / s + 4 + part * s;
     if (time < least) {
       least = time;
       best = s;
@@ -140,15 +144,15 @@ static int pre_splits(const CacheView& c, int max_new) {
   return best;
 }
 
-long long prefill_scratch_bytes(const CacheView& c, int max_new) {
-  const int ns = pre_splits(c, max_new);
+long long prefill_scratch_bytes(const CacheView& c, int max_new, bool four_bits) {
+  const int ns = pre_splits(c, max_new, four_bits);
   return ns == 1 ? 0 : 4ll * c.n_seq * max_new * c.hq * ns * (c.dh + 2);
 }
 
-PreScratch pre_plan(const CacheView& c, int max_new, void* scratch, int* row_blocks) {
+PreScratch pre_plan(const CacheView& c, int max_new, bool four_bits, void* scratch, int* row_blocks) {
   PreScratch sc{};
   *row_blocks = pre_row_blocks(c, max_new);
-  sc.nsplit = pre_splits(c, max_new);
+  sc.nsplit = pre_splits(c, max_new, four_bits);
   if (sc.nsplit > 1) {
     sc.part = static_cast<float*>(scratch);
     sc.ml = sc.part + static_cast<long long>(c.n_seq) * max_new * c.hq * sc.nsplit * c.dh;
@@ -168,7 +172,7 @@ hipError_t launch_prefill_join(const CacheView& c, const AttendArgs& a, const Pr
 
 hipError_t launch_cache_prefill(const CacheView& c, const AttendArgs& a, void* scratch, hipStream_t st) {
   int row_blocks;
-  const PreScratch sc = pre_plan(c, a.max_new, scratch, &row_blocks);
+  const PreScratch sc = pre_plan(c, a.max_new, false, scratch, &row_blocks);
 #define GMC_PREFILL(T, DH)                                                                                       \
   case DH:                                                                                                       \
     hipLaunchKernelGGL((prefill_kernel<T, DH>), dim3(static_cast<unsigned>(sc.grid.blocks)), dim3(64 * kPreWaves), 0, st, c, a, sc, \
