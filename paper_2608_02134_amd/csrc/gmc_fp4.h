@@ -44,4 +44,35 @@ __device__ __forceinline__ uint32_t fp4_codes(const float* x, float scale) {
   return u;
 }
 
+// fp32 beside values of 4 bits, which are bf16: x as the upper 8 significant bits,
+// the next 8, and the rest rounded.  Infinities and NaN are all in the first part.
+__device__ __forceinline__ __bf16 upper_half(uint32_t u) {
+  return __builtin_bit_cast(__bf16, static_cast<uint16_t>(u >> 16));
+}
+__device__ __forceinline__ void split3(float x, __bf16* part) {
+  const uint32_t u = __float_as_uint(x);
+  const bool finite = (u & 0x7F800000u) != 0x7F800000u;
+  const float rest = finite ? x - __uint_as_float(u & 0xFFFF0000u) : 0.f;
+  const uint32_t v = __float_as_uint(rest) & 0xFFFF0000u;
+  part[0] = finite ? upper_half(u) : static_cast<__bf16>(x);
+  part[1] = upper_half(v);
+  part[2] = static_cast<__bf16>(rest - __uint_as_float(v));
+}
+
+// A weight (not negative) as two or three parts, none of which is zero if it is
+// not: an infinite value, which scales from 2^126 on have, stays what it is.
+__device__ __forceinline__ void split2_weight(float e, __bf16* part) {
+  const uint32_t u = __float_as_uint(e) & 0xFFFF0000u;
+  part[0] = upper_half(u);
+  part[1] = static_cast<__bf16>(fmaxf(e - __uint_as_float(u), e * 0x1p-24f));
+}
+__device__ __forceinline__ void split3_weight(float e, __bf16* part) {
+  const uint32_t u = __float_as_uint(e) & 0xFFFF0000u;
+  const float rest = e - __uint_as_float(u);
+  const uint32_t v = __float_as_uint(fmaxf(rest, e * 0x1p-25f)) & 0xFFFF0000u;
+  part[0] = upper_half(u);
+  part[1] = upper_half(v);
+  part[2] = static_cast<__bf16>(fmaxf(rest - __uint_as_float(v), e * 0x1p-33f));
+}
+
 }  // namespace gmc

@@ -5,6 +5,7 @@
 #include <limits.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "gmc_cache.h"
 #include "gmc_cache_grid.h"
@@ -93,13 +94,18 @@ struct PreScratch {
 // Splits that a block's tiles are shared over: none with fewer than two tiles.
 __device__ __forceinline__ int used_pre_splits(int tiles, int nsplit) { return min(nsplit, max(1, tiles / 2)); }
 
-// Q4: the pages hold 4 bits, whose values a tile in shared memory holds as T.
+// Q4: the pages hold 4 bits, whose values a tile in shared memory holds as bf16,
+// exactly.  Queries of T and the weights enter as kParts bf16 each, fp32 ones as
+// three (24 bits): six matrix products of bf16 in the place of two of fp32, which are
+// an eighth as fast.
 template <typename T, int DH, bool Q4>
 __device__ __forceinline__ void prefill_block(const CacheView& c, const CacheScales& s4, const AttendArgs& a,
                                               const PreScratch& sc, int row_blocks) {
-  using KTile = KeyTile<T, DH>;
+  using E = std::conditional_t<Q4, bf16_t, T>;   // what a tile holds
+  constexpr int kParts = Q4 && std::is_same_v<T, float> ? 3 : 1;
+  using KTile = KeyTile<E, DH>;
   constexpr int CPR = KTile::CPR, KT = KTile::KT, KB = KT / 32, NB = DH / 32, PITCH = CPR * 16;
-  constexpr int NS = sizeof(T) == 2 ? DH / 16 : DH / 8;    // reads of 16 bytes a lane needs of its K row
+  constexpr int NS = sizeof(E) == 2 ? DH / 16 : DH / 8;    // reads of 16 bytes a lane needs of its K row
   constexpr int GROUPS = KT / 16;                          // runs of 16 slots, each on one page
   constexpr int LOADS = CPR / 4;                           // 1 KB loads of one run
   __shared__ __align__(16) unsigned char k_even[KT * PITCH], v_even[KT * PITCH], k_odd[KT * PITCH], v_odd[KT * PITCH];
@@ -158,11 +164,27 @@ __device__ __forceinline__ void prefill_block(const CacheView& c, const CacheSca
   };
   const int ids0 = fetch(it0), ids1 = fetch(it0 + 1);
 
-  uint4 q[NS];
+  uint4 q[kParts][NS];
   {
     const T* qp = static_cast<const T*>(a.q) + (wk.first + tok) * a.q_stride + static_cast<long long>(hq) * DH;
 #pragma unroll
-    for (int s = 0; s < NS; ++s) q[s] = ld16(reinterpret_cast<const char*>(qp) + 16 * (2 * s + half));
+    for (int s = 0; s < NS; ++s) {
+      if constexpr (kParts == 1) {
+        q[0][s] = ld16(reinterpret_cast<const char*>(qp) + 16 * (2 * s + half));
+      } else {
+        const Frag<float> f = frag_load<float>(reinterpret_cast<const float*>(qp) + 8 * (2 * s + half));
+        bf16x8 y[3];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          __bf16 part[3];
+          split3(f.v[e], part);
+#pragma unroll
+          for (int u = 0; u < 3; ++u) y[u][e] = part[u];
+        }
+#pragma unroll
+        for (int u = 0; u < 3; ++u) q[kParts > 1 ? u : 0][s] = __builtin_bit_cast(uint4, y[u]);
+      }
+    }
   }
   floatx16 o[NB];
 #pragma unroll
@@ -182,7 +204,7 @@ __device__ __forceinline__ void prefill_block(const CacheView& c, const CacheSca
     return r * PITCH + KTile::chunk_at(r, p % CPR) * 16;
   };
   constexpr bool kXor = KTile::kPow2;
-  constexpr int VO = sizeof(T) == 2 ? 2 : 4;
+  constexpr int VO = sizeof(E) == 2 ? 2 : 4;
   int k_base[kXor ? 1 : NS], v_base[kXor ? 1 : NB][VO];
 #pragma unroll
   for (int s = 0; s < (kXor ? 1 : NS); ++s) k_base[s] = col * PITCH + KTile::place(col, 2 * s + half) * 16;
@@ -190,7 +212,7 @@ __device__ __forceinline__ void prefill_block(const CacheView& c, const CacheSca
   for (int n = 0; n < (kXor ? 1 : NB); ++n)
 #pragma unroll
     for (int e = 0; e < VO; ++e) {
-      if constexpr (sizeof(T) == 2) {      // a transposing read of 4 keys x 16 dims
+      if constexpr (sizeof(E) == 2) {      // a transposing read of 4 keys x 16 dims
         const int i = lane & 15, r = 8 * e + 4 * half + (i >> 2);
         const int ch = 4 * n + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
         v_base[n][e] = r * PITCH + KTile::place(r, ch) * 16 + 8 * (i & 1);
@@ -201,7 +223,7 @@ __device__ __forceinline__ void prefill_block(const CacheView& c, const CacheSca
     }
   auto k_off = [&](int s) GMC_INLINE { return kXor ? k_base[0] ^ (32 * s) : k_base[kXor ? 0 : s]; };
   auto v_off = [&](int n, int e) GMC_INLINE {
-    return kXor ? v_base[0][e] ^ ((sizeof(T) == 2 ? 64 : 128) * n) : v_base[kXor ? 0 : n][e];
+    return kXor ? v_base[0][e] ^ ((sizeof(E) == 2 ? 64 : 128) * n) : v_base[kXor ? 0 : n][e];
   };
 
   const long long page_bytes = static_cast<long long>(c.page) * PITCH;
@@ -245,14 +267,14 @@ __device__ __forceinline__ void prefill_block(const CacheView& c, const CacheSca
   // Sets the infinities and NaN among a lane's 16 bytes of values to zero; returns
   // whether there were any.
   auto clean = [](u32x4& y) GMC_INLINE {
-    constexpr uint32_t kExp = sizeof(T) == 2 ? 0x7F807F80u : 0x7F800000u, kOne = sizeof(T) == 2 ? 0x00800080u : 0x00800000u;
-    constexpr uint32_t kTop = sizeof(T) == 2 ? 0x80008000u : 0x80000000u;
+    constexpr uint32_t kExp = sizeof(E) == 2 ? 0x7F807F80u : 0x7F800000u, kOne = sizeof(E) == 2 ? 0x00800080u : 0x00800000u;
+    constexpr uint32_t kTop = sizeof(E) == 2 ? 0x80008000u : 0x80000000u;
     const uint32_t hit = (((y.x & kExp) + kOne) | ((y.y & kExp) + kOne) | ((y.z & kExp) + kOne) | ((y.w & kExp) + kOne)) & kTop;
     if (!hit) return false;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const uint32_t top = ((y[e] & kExp) + kOne) & kTop;   // a bit for each value that goes
-      y[e] = sizeof(T) == 2 ? y[e] & ~((top >> 15) * 0xFFFFu) : (top ? 0u : y[e]);
+      y[e] = sizeof(E) == 2 ? y[e] & ~((top >> 15) * 0xFFFFu) : (top ? 0u : y[e]);
     }
     return true;
   };
@@ -294,7 +316,7 @@ __device__ __forceinline__ void prefill_block(const CacheView& c, const CacheSca
 #pragma unroll
       for (int i = 0; i < 16; ++i) x[kb][i] = 0.f;
     typedef __attribute__((address_space(3))) shortx4 shared4;
-    if constexpr (sizeof(T) == 2) {
+    if constexpr (sizeof(E) == 2) {
       // kAhead steps of K's reads before the first product, then one step of
       // products for one of reads
       constexpr int kAhead = NS < 4 ? NS : 4;
@@ -306,21 +328,23 @@ __device__ __forceinline__ void prefill_block(const CacheView& c, const CacheSca
 #pragma unroll
       for (int s = 0; s < NS; ++s)
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
-          x[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[s][kb]),
-                                                          __builtin_bit_cast(bf16x8, q[s]), x[kb], 0, 0, 0);
+        for (int part = kParts - 1; part >= 0; --part)
+#pragma unroll
+          for (int kb = 0; kb < KB; ++kb)
+            x[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[s][kb]),
+                                                            __builtin_bit_cast(bf16x8, q[part][s]), x[kb], 0, 0, 0);
       __builtin_amdgcn_sched_group_barrier(0x100, kAhead * KB, 0);
 #pragma unroll
       for (int s = 0; s < NS - kAhead; ++s) {
-        __builtin_amdgcn_sched_group_barrier(0x8, KB, 0);
+        __builtin_amdgcn_sched_group_barrier(0x8, kParts * KB, 0);
         __builtin_amdgcn_sched_group_barrier(0x100, KB, 0);
       }
-      __builtin_amdgcn_sched_group_barrier(0x8, kAhead * KB, 0);
+      __builtin_amdgcn_sched_group_barrier(0x8, kAhead * kParts * KB, 0);
     } else {
 #pragma unroll
       for (int s = 0; s < NS; ++s) {
         const u32x4 kf = ld_shared<u32x4>(ks + k_off(s));
-        const uint32_t qe[4] = {q[s].x, q[s].y, q[s].z, q[s].w};
+        const uint32_t qe[4] = {q[0][s].x, q[0][s].y, q[0][s].z, q[0][s].w};
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           x[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[e]), __uint_as_float(qe[e]), x[0], 0, 0, 0);
@@ -390,7 +414,7 @@ __device__ __forceinline__ void prefill_block(const CacheView& c, const CacheSca
       x[kb][i] = __builtin_amdgcn_exp2f(fmaf(x[kb][i], cs, -base));
       sum += x[kb][i];
     };
-    if constexpr (sizeof(T) == 2) {
+    if constexpr (sizeof(E) == 2) {
       // 16 keys at a time: their products are spread over the exponentials of
       // the next 16 keys, whose values are read meanwhile
       shortx4 v[2][NB][2];
@@ -401,12 +425,20 @@ __device__ __forceinline__ void prefill_block(const CacheView& c, const CacheSca
           for (int e = 0; e < 2; ++e)
             v[st % 2][n][e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((shared4*)(vs + 16 * st * PITCH + v_off(n, e)));
       };
-      bf16x8 p[2];
+      bf16x8 p[2][kParts];
       auto weights = [&](int st) GMC_INLINE {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           weight(st / 2, 8 * (st % 2) + j);
-          p[st % 2][j] = static_cast<__bf16>(x[st / 2][8 * (st % 2) + j]);
+          const float y = x[st / 2][8 * (st % 2) + j];
+          if constexpr (kParts == 1) {
+            p[st % 2][0][j] = static_cast<__bf16>(y);
+          } else {
+            __bf16 part[3];
+            split3_weight(y, part);
+#pragma unroll
+            for (int u = 0; u < 3; ++u) p[st % 2][kParts > 1 ? u : 0][j] = part[u];
+          }
         }
       };
       read_values(0);
@@ -416,7 +448,9 @@ __device__ __forceinline__ void prefill_block(const CacheView& c, const CacheSca
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
           const auto both = __builtin_shufflevector(v[st % 2][n][0], v[st % 2][n][1], 0, 1, 2, 3, 4, 5, 6, 7);
-          o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, both), p[st % 2], o[n], 0, 0, 0);
+#pragma unroll
+          for (int part = kParts - 1; part >= 0; --part)
+            o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, both), p[st % 2][part], o[n], 0, 0, 0);
         }
         if (st + 1 < 2 * KB) {
           read_values(st + 1);
@@ -504,14 +538,7 @@ __device__ __forceinline__ void prefill_block(const CacheView& c, const CacheSca
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const uint4 y = fp4_words(codes[e], f);
-        if constexpr (sizeof(T) == 2) {
-          *reinterpret_cast<shared_u32x4*>(to + 16 * KTile::place(r, 4 * blk + e)) = u32x4{y.x, y.y, y.z, y.w};
-        } else {
-          *reinterpret_cast<shared_u32x4*>(to + 16 * KTile::place(r, 8 * blk + 2 * e)) =
-              u32x4{y.x << 16, y.x & 0xFFFF0000u, y.y << 16, y.y & 0xFFFF0000u};
-          *reinterpret_cast<shared_u32x4*>(to + 16 * KTile::place(r, 8 * blk + 2 * e + 1)) =
-              u32x4{y.z << 16, y.z & 0xFFFF0000u, y.w << 16, y.w & 0xFFFF0000u};
-        }
+        *reinterpret_cast<shared_u32x4*>(to + 16 * KTile::place(r, 4 * blk + e)) = u32x4{y.x, y.y, y.z, y.w};
       }
     }
     __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0): the codes have been read before the next ones come
@@ -531,9 +558,14 @@ __device__ __forceinline__ void prefill_block(const CacheView& c, const CacheSca
       if (it0 < it1) ok0 = issue(it0, ids0, kb0, vb0, pb0);
     }
     if (!care && a.scale < 0.f) {
-      constexpr uint32_t kFlip = sizeof(T) == 2 ? 0x80008000u : 0x80000000u;
+      constexpr uint32_t kFlip = sizeof(E) == 2 ? 0x80008000u : 0x80000000u;
 #pragma unroll
-      for (int s = 0; s < NS; ++s) { q[s].x ^= kFlip; q[s].y ^= kFlip; q[s].z ^= kFlip; q[s].w ^= kFlip; }
+      for (int part = 0; part < kParts; ++part)
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+          uint4& y = q[part][s];
+          y.x ^= kFlip; y.y ^= kFlip; y.z ^= kFlip; y.w ^= kFlip;
+        }
     }
     int ids = ids1;
     if constexpr (Q4) {

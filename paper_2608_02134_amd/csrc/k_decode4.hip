@@ -53,18 +53,6 @@ __device__ __forceinline__ uint32_t scale_at_bits(uint32_t bytes, int n) {
 }
 __device__ __forceinline__ float scale_at(uint32_t bytes, int n) { return __uint_as_float(scale_at_bits(bytes, n)); }
 
-// x as bf16 parts: the upper 8 significant bits, the next 8, and the rest rounded.
-// Infinities and NaN are all in the first part.
-__device__ __forceinline__ void split3(float x, __bf16* hi, __bf16* mid, __bf16* lo) {
-  const uint32_t u = __float_as_uint(x);
-  const bool finite = (u & 0x7F800000u) != 0x7F800000u;
-  const float h = __uint_as_float(u & 0xFFFF0000u), rest = finite ? x - h : 0.f;
-  const float m = __uint_as_float(__float_as_uint(rest) & 0xFFFF0000u);
-  *hi = finite ? __builtin_bit_cast(__bf16, static_cast<uint16_t>(u >> 16)) : static_cast<__bf16>(x);
-  *mid = __builtin_bit_cast(__bf16, static_cast<uint16_t>(__float_as_uint(m) >> 16));
-  *lo = static_cast<__bf16>(rest - m);
-}
-
 // Shared and global memory by their address spaces, as loads into shared memory
 // take them.
 typedef __attribute__((address_space(3))) uint8_t shared_u8;
@@ -213,9 +201,9 @@ decode4_kernel(CacheView c, CacheScales sc4, AttendArgs a, DecodeScratch sc, int
             for (int e = 0; e < 8; ++e) f.v[e] = -f.v[e];
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            __bf16 x0, x1, x2;
-            split3(f.v[e], &x0, &x1, &x2);
-            q[0][s][e] = x0; q[1][s][e] = x1; q[2][s][e] = x2;
+            __bf16 part[3];
+            split3(f.v[e], part);
+            q[0][s][e] = part[0]; q[1][s][e] = part[1]; q[2][s][e] = part[2];
           }
         }
       }
@@ -304,18 +292,11 @@ decode4_kernel(CacheView c, CacheScales sc4, AttendArgs a, DecodeScratch sc, int
         const float e = __builtin_amdgcn_exp2f(fmaf(x[hh][r], cs, -base));
         l += e;   // this lane group's keys; joined at the end
         const int at = 4 * hh + r;
-        // (no part of a weight above zero is zero: an infinite value, which scales
-        // from 2^126 on have, stays what it is)
-        const uint32_t u = __float_as_uint(e) & 0xFFFF0000u;
-        const float rest = e - __uint_as_float(u);
-        p[0][at] = __builtin_bit_cast(__bf16, static_cast<uint16_t>(u >> 16));
-        if constexpr (NP == 2) {
-          p[1][at] = static_cast<__bf16>(fmaxf(rest, e * 0x1p-24f));
-        } else {
-          const uint32_t v = __float_as_uint(fmaxf(rest, e * 0x1p-25f)) & 0xFFFF0000u;
-          p[1][at] = __builtin_bit_cast(__bf16, static_cast<uint16_t>(v >> 16));
-          p[2][at] = static_cast<__bf16>(fmaxf(rest - __uint_as_float(v), e * 0x1p-33f));
-        }
+        __bf16 part[3];
+        if constexpr (NP == 2) split2_weight(e, part);
+        else split3_weight(e, part);
+#pragma unroll
+        for (int y = 0; y < NP; ++y) p[y][at] = part[y];
       }
     uint32_t sv[H][SB];
 #pragma unroll

@@ -108,7 +108,9 @@ prefill_join_kernel(CacheView c, AttendArgs a, PreScratch sc) {
     a.lse[row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
-static int pre_key_tile(const CacheView& c) { return c.dtype != 0 && c.dh <= 128 ? 64 : 32; }
+static int pre_key_tile(const CacheView& c, bool four_bits) {
+  return (c.dtype != 0 || four_bits) && c.dh <= 128 ? 64 : 32;
+}
 
 static int pre_row_blocks(const CacheView& c, int max_new) {
   return static_cast<int>((static_cast<long long>(max_new) * c.hg + kPreRows - 1) / kPreRows);
@@ -127,9 +129,9 @@ static int pre_row_blocks(const CacheView& c, int max_new) {
 // 4100 slots 29.8 us with 240 blocks, 32.4 with 280; three such requests 43.7 with 480, 57
 // with 240; 16 over 32768 35.6 with 256, 38.6 with 348).
 static int pre_splits(const CacheView& c, int max_new, bool four_bits) {
-  const int kt = pre_key_tile(c), tiles = (c.cap + kt - 1) / kt;
+  const int kt = pre_key_tile(c, four_bits), tiles = (c.cap + kt - 1) / kt;
   const long long blocks = static_cast<long long>(pre_row_blocks(c, max_new)) * c.hkv * c.n_seq;
-  const double tile = (c.dtype == 0 ? 1.9 / (32 * 64) : 1.7 / (64 * 128)) * kt * c.dh;
+  const double tile = (c.dtype != 0 ? 1.7 / (64 * 128) : four_bits ? 3.0 / (64 * 128) : 1.9 / (32 * 64)) * kt * c.dh;
   const double part = 8e-6 / 4 * (c.dh + 2) * c.hq * max_new * c.n_seq;
   int best = 1;
   double least = tile * tiles;

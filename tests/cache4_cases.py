@@ -84,8 +84,8 @@ def rotary_on_gpu(r):
 
 
 def check_attention(ref, out, lse, dtype, dh, decode):
-    """C.check_attention, whose sums have a term for each product: decode's
-    products enter as up to three terms (bf16 weights two, fp32 queries and weights
-    three), which are exact, and the sums have as many more additions."""
-    terms = 1 if not decode else 2 if dtype == "bf16" else 3
+    """C.check_attention, whose sums have a term for each product: bf16 weights of
+    decode enter as two terms, fp32 queries and weights as three, which are exact, and
+    the sums have as many more additions."""
+    terms = 3 if dtype == "f32" else 2 if decode else 1
     C.check_attention({**ref, "most": ref["most"] * terms}, out, lse, dtype, dh if dtype == "bf16" else dh * terms)
