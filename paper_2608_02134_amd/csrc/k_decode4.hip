@@ -5,10 +5,11 @@
 // of 512: bound by memory where the caches are long, if enough loads are on their way
 // and the instructions beside them are few.
 //   Loads: tiles of 32 keys go from the pages into shared memory without registers
-//      between, each wave its own, two tiles ahead of the one it computes: five loads
-//      a tile of 128 dims.  (Into registers, 14 loads a tile, one tile ahead: 278 us where
-//      this takes 198; loads alone take 182.)  What a lane loads is what it reads back,
-//      where K is concerned; V is turned by the addresses of the reads.
+//      between, each wave its own, one tile ahead of the one it computes: five loads
+//      a tile of 128 dims.  (Into registers, 14 loads a tile: 278 us where this takes 197;
+//      loads alone take 179.  Two tiles ahead were 199, four waves a SIMD 233, with
+//      spilt registers.)  What a lane loads is what it reads back, where K is
+//      concerned; V is turned by the addresses of the reads.
 //   K: the order of the elements in a product is free, so lane (key l % 16, group g =
 //      l / 16) takes a run of them: of each 128 the 32 from 32 g, one block with one
 //      scale; of what is left 16 from 16 g (64) and 8 from 8 g (32).
@@ -83,11 +84,8 @@ template <int N> __device__ __forceinline__ void arrive() {   // until at most N
   asm volatile("" ::: "memory");
 }
 
-// Tiles a wave has in shared memory: the one it computes and those on their way.
-// Three blocks of four waves to a CU find room with heads of up to 128, two with
-// wider ones and in fp32 with 96 to 160, one in fp32 from 192 on, whose registers are
-// more.
-template <int DH, int WAVES> constexpr int kRing = DH <= 128 && WAVES == kDecodeWaves ? 3 : 2;
+// Three blocks of four waves to a CU with heads of up to 128, two with wider ones and
+// in fp32 with 96 to 160, one in fp32 from 192 on, whose registers are more.
 constexpr int blocks_of_cu(int type_bytes, int dh, int waves) {
   return type_bytes == 4 && dh > 160 ? 1 : dh <= (type_bytes == 2 ? 128 : 64) && waves == kDecodeWaves ? 3 : 2;
 }
@@ -99,11 +97,9 @@ decode4_kernel(CacheView c, CacheScales sc4, AttendArgs a, DecodeScratch sc, int
   constexpr int H = 2, TK = kTile4, NS = DH / 32, NO = DH / 16, ROW = DH / 2;
   constexpr int SB = scale_bytes(DH);
   constexpr int NQ = sizeof(T) == 2 ? 1 : 3, NP = sizeof(T) == 2 ? 2 : 3;   // bf16 parts of queries and weights
-  constexpr int kTiles = kRing<DH, WAVES>;
-  __shared__ __align__(16) uint8_t ring0[WAVES * L::kBytes], ring1[WAVES * L::kBytes];
-  __shared__ __align__(16) uint8_t ring2[kTiles > 2 ? WAVES * L::kBytes : 16];
+  __shared__ __align__(16) uint8_t even[WAVES * L::kBytes], odd[WAVES * L::kBytes];
   __shared__ float stat[WAVES][2][16];
-  static_assert(sizeof(ring0) >= WAVES / 2 * 16 * DH * sizeof(float), "the waves' parts take the first tiles' place");
+  static_assert(sizeof(even) >= WAVES / 2 * 16 * DH * sizeof(float), "the waves' parts take the first tiles' place");
   const int split = blockIdx.x, h = blockIdx.y / qtiles, qt = blockIdx.y % qtiles, b = blockIdx.z;
   const int lane = threadIdx.x & 63, w = wave_id(), i16 = lane & 15, g = lane >> 4;
   const int len = cache_len(c, b);
@@ -369,11 +365,11 @@ decode4_kernel(CacheView c, CacheScales sc4, AttendArgs a, DecodeScratch sc, int
     }
   };
 
-  // Page ids come one tile before their loads.
-  shared_u8* const at0 = (shared_u8*)ring0 + w * L::kBytes;
-  shared_u8* const at1 = (shared_u8*)ring1 + w * L::kBytes;
-  shared_u8* const at2 = kTiles > 2 ? (shared_u8*)ring2 + w * L::kBytes : at0;
-  unsigned ok0 = 0, ok1 = 0, ok2 = 0;
+  // One tile is computed while the next one's loads are on their way; its page ids
+  // come one tile before.
+  shared_u8* const at0 = (shared_u8*)even + w * L::kBytes;
+  shared_u8* const at1 = (shared_u8*)odd + w * L::kBytes;
+  unsigned ok0 = 0, ok1 = 0;
   int tile = t0 + w, id[H];
   auto next = [&](int t, unsigned* ok, shared_u8* to) __attribute__((always_inline)) {
     if (t >= t1) return;
@@ -382,40 +378,26 @@ decode4_kernel(CacheView c, CacheScales sc4, AttendArgs a, DecodeScratch sc, int
     issue(t, id, *ok, to);
     ids_of(t + WAVES, id);
   };
-  // the tile t while those behind it are on their way
   auto step = [&](int t, unsigned ok, const shared_u8* in) __attribute__((always_inline)) {
-    if (kTiles > 2 && t + 2 * WAVES < t1) arrive<2 * L::kInFlight>();
-    else if (t + WAVES < t1) arrive<L::kInFlight>();
+    if (t + WAVES < t1) arrive<L::kInFlight>();   // those of the next tile may still be on their way
     else arrive<0>();
     compute(t, ok, in);
   };
   if (tile < t1) {
     ids_of(tile, id);
     next(tile, &ok0, at0);
-    if constexpr (kTiles > 2) next(tile + WAVES, &ok1, at1);
   }
-  for (; tile < t1; tile += kTiles * WAVES) {
-    if constexpr (kTiles > 2) {
-      next(tile + 2 * WAVES, &ok2, at2);
-      step(tile, ok0, at0);
-      if (tile + WAVES >= t1) break;
-      next(tile + 3 * WAVES, &ok0, at0);
-      step(tile + WAVES, ok1, at1);
-      if (tile + 2 * WAVES >= t1) break;
-      next(tile + 4 * WAVES, &ok1, at1);
-      step(tile + 2 * WAVES, ok2, at2);
-    } else {
-      next(tile + WAVES, &ok1, at1);
-      step(tile, ok0, at0);
-      if (tile + WAVES >= t1) break;
-      next(tile + 2 * WAVES, &ok0, at0);
-      step(tile + WAVES, ok1, at1);
-    }
+  for (; tile < t1; tile += 2 * WAVES) {
+    next(tile + WAVES, &ok1, at1);
+    step(tile, ok0, at0);
+    if (tile + WAVES >= t1) break;
+    next(tile + 2 * WAVES, &ok0, at0);
+    step(tile + WAVES, ok1, at1);
   }
   asm volatile("s_nop 15\n\ts_nop 7" ::: "memory");   // (see settle)
   __builtin_amdgcn_sched_barrier(0);
   m = m * cs;          // (as the parts' maxima are joined)
-  float(*const red)[16 * DH] = reinterpret_cast<float(*)[16 * DH]>(ring0);
+  float(*const red)[16 * DH] = reinterpret_cast<float(*)[16 * DH]>(even);
 
   // the waves' parts on their common maximum, added in a fixed order
   l = add_xor32(add_xor16(l));
