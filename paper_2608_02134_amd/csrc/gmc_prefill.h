@@ -569,8 +569,8 @@ __device__ __forceinline__ void prefill_block(const CacheView& c, const CacheSca
     }
     int ids = ids1;
     if constexpr (Q4) {
-      // (a tile's values go to shared memory when those before it have been
-      // computed by all waves, and the next one's codes into the registers)
+      // (the next tile's values are formed after this one's products: 16448 tokens
+      // 1004 us, before them 1034; half of the blocks so and half so 1031)
       if (it0 < it1) {
         spread4(kb0, vb0);
         if (it0 + 1 < it1) ok1 = fetch4(it0 + 1, ids);
@@ -579,21 +579,21 @@ __device__ __forceinline__ void prefill_block(const CacheView& c, const CacheSca
       for (int it = it0; it < it1; it += 2) {
         __syncthreads();
         unsigned ok2 = 0;
+        compute(it, ok0, kb0, vb0, pb0);
         if (it + 1 < it1) {
           spread4(kb1, vb1);
           if (it + 2 < it1) ok2 = fetch4(it + 2, ids);
           ids = fetch(it + 3);
         }
-        compute(it, ok0, kb0, vb0, pb0);
         ok0 = ok2;
         if (it + 1 >= it1) break;
         __syncthreads();
+        compute(it + 1, ok1, kb1, vb1, pb1);
         if (it + 2 < it1) {
           spread4(kb0, vb0);
           if (it + 3 < it1) ok2 = fetch4(it + 3, ids);
           ids = fetch(it + 4);
         }
-        compute(it + 1, ok1, kb1, vb1, pb1);
         ok1 = ok2;
       }
     }

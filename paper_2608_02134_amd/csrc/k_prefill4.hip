@@ -4,7 +4,7 @@
 // shared memory serves 128 rows, so its values are formed once, as bf16, between the
 // pages and shared memory, while the codes of the next tile are on their way to a place
 // of their own there.  A tile so costs a thread 32 conversions and 8 writes more than
-// one of bf16 pages: 16448 tokens, window 4096, 28 heads on 4 of 128 in bf16 1.03 ms, 815
+// one of bf16 pages: 16448 tokens, window 4096, 28 heads on 4 of 128 in bf16 1.00 ms, 845
 // TFLOP/s (bf16 pages 0.96 on the same card).
 // fp32 queries and weights enter as three bf16 (gmc_prefill.h): 4096 tokens, 28 heads
 // on 4 of 128, 0.63 ms; products of fp32 took 1.82.

@@ -8,6 +8,11 @@
 // own: the second load is the cache's).  A lane keeps its piece over all heads of
 // a token, so that it reads its cosines and sines once.  Four neighbouring lanes
 // have a block of 32: its largest magnitude takes two exchanges.
+//
+// 16448 tokens, 28 query heads on 4 of 128 in bf16: 54 us, 5.6 TB/s.  16 prompts of
+// 335 rows picked from 1375 into 4 bits, 4 heads of 128: 9.9 us, of which most are five
+// trips to memory one after the other (pick, position, table, page, rows).  One token
+// of 16 sequences with 28 query heads 5.0 us.
 #include <algorithm>
 
 #include "gmc_cache.h"
@@ -253,7 +258,8 @@ hipError_t launch_cache_append_rotary(const CacheView& c, const CacheScales* sca
 }
 
 // --- rows of 4 bits back --------------------------------------------------------
-// A wave a token; a lane turns a word of eight codes into eight values.
+// A wave a token; a lane turns a word of eight codes into eight values (16 x 335
+// rows of 4 heads of 128 in bf16: 6.4 us).
 template <typename T>
 __global__ void __launch_bounds__(256)
 cache4_read_kernel(CacheView c, CacheScales sc, long long rows, const int32_t* starts, int max_new, T* k_out, T* v_out) {

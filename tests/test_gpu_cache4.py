@@ -564,7 +564,7 @@ def test_sequences_that_share_pages():
     _prefill(rng, c, [10, 30, 48], 0, 0)
 
 
-@pytest.mark.parametrize("n_seq,hkv,new", [(65535, 8, 1), (300, 24, 2)])
+@pytest.mark.parametrize("n_seq,hkv,new", [(65535, 8, 1), (300, 24, 2), (65535, 1, 11)])
 def test_many_sequences(n_seq, hkv, new):
     """As many sequences as a call takes: every one's rows as one sequence alone has them."""
     _say(f"4 bits, {n_seq} sequences")

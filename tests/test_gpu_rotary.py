@@ -135,6 +135,27 @@ def test_queries_in_place(n, dtype):
         assert C.same(C.host(x), C.rounded(O4.turn(q, r, 2 + np.arange(n)), dtype)), shape
 
 
+@pytest.mark.parametrize("n", [8, 9, 256, 257])
+def test_few_and_many_tokens(n):
+    """Tokens that one block takes, those whose heads four waves share and those that a
+    wave has to itself: as one token at a time."""
+    _say(f"append_rotary of {n} tokens")
+    rng = np.random.default_rng(n)
+    args = dict(dtype="bf16", hq=12, hkv=4, dh=96, page=32, lens=[3, 40], slots=304)
+    a, b = (C.on_gpu(C.make(np.random.default_rng(5), **args)) for _ in range(2))
+    r = C4.rotary_on_gpu(C4.rotary(rng, 400, 96))
+    x = C.to_gpu(C.rounded(rng.standard_normal((2, n, 20, 96)), "bf16"), "bf16")
+    y = x.view(2 * n, 20, 96).clone()
+    q = y[:, :12].contiguous()
+    got = a.append_rotary(y[:, 12:16], y[:, 16:], r, q=q, out=q).view(2, n, 12, 96)
+    for i in range(n):
+        one = x[:, i].contiguous()
+        want = b.append_rotary(one[:, 12:16], one[:, 16:], r, q=one[:, :12])
+        assert torch.equal(got[:, i], want), i
+    for name in ("k_pages", "v_pages", "lens"):
+        assert torch.equal(torch.nan_to_num(getattr(a, name).float()), torch.nan_to_num(getattr(b, name).float())), name
+
+
 @pytest.mark.parametrize("n", [6, 26])
 def test_full_caches_and_bad_indices(n):
     """Tokens past the capacity are not stored, rows on pages that are none left
