@@ -23,9 +23,9 @@
 // fp32; weights for bf16 outputs as two (16 bits).  The matrix cores idle, so this
 // costs nothing.
 //
-// 8 requests of 100000 to 131072 slots, 32 heads on 8 of 128 in bf16: 193 us, 5.2
-// TB/s (of bf16 pages 633).  64 requests of 200 to 4096 slots, 28 heads on 4: 26 us
-// with the joining kernel.
+// 8 requests of 100000 to 131072 slots, 32 heads on 8 of 128 in bf16: 190 us, 5.3
+// TB/s, and 5 for the joining kernel (over bf16 pages 633).  64 requests of 200 to 4096
+// slots, 28 heads on 4: 20 us and 4.
 #include <algorithm>
 
 #include "gmc_cache.h"
@@ -459,11 +459,11 @@ decode4_kernel(CacheView c, CacheScales sc4, AttendArgs a, DecodeScratch sc, int
 
 static int decode4_qtiles(const CacheView& c) { return (c.hg + 15) / 16; }
 
-// As many blocks as find room on the chip together, three to a CU (us with 512, 768,
-// 1024 and 1536: 8 requests of 100000 to 131072 slots, 32 heads on 8 of 128, 205, 200, 197 and
-// 194; 64 of 200 to 4096, 28 on 4, 28.2, 26.3, 27.5 and 28; 16 of them 13.0, 13.8, 15.4
-// and 17).  Splits of one length for all sequences, so that short ones have fewer, were
-// slower: 210 and 28.1.
+// As many blocks as find room on the chip together, three to a CU (with two tiles
+// ahead, us with 512, 768, 1024 and 1536: 8 requests of 100000 to 131072 slots, 32 heads on
+// 8 of 128, 205, 200, 197 and 194; 64 of 200 to 4096, 28 on 4, 28.2, 26.3, 27.5 and 28; 16 of
+// them 13.0, 13.8, 15.4 and 17).  Splits of one length for all sequences, so that short ones
+// have fewer, were slower: 210 and 28.1.
 constexpr int kDecode4Blocks = 768;
 static int decode4_splits(const CacheView& c, int qtiles) {
   const long long groups = static_cast<long long>(c.n_seq) * c.hkv * qtiles;
