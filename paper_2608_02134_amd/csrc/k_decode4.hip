@@ -84,6 +84,13 @@ template <int N> __device__ __forceinline__ void arrive() {   // until at most N
   asm volatile("" ::: "memory");
 }
 
+// As many blocks as find room on the chip together, three to a CU (with two tiles
+// ahead, us with 512, 768, 1024 and 1536: 8 requests of 100000 to 131072 slots, 32 heads on
+// 8 of 128, 205, 200, 197 and 194; 64 of 200 to 4096, 28 on 4, 28.2, 26.3, 27.5 and 28; 16 of
+// them 13.0, 13.8, 15.4 and 17).  Splits of one length for all sequences, so that short ones
+// have fewer, were slower: 210 and 28.1.
+constexpr int kDecode4Blocks = 768;
+
 // Three blocks of four waves to a CU with heads of up to 128, two with wider ones and
 // in fp32 with 96 to 160, one in fp32 from 192 on, whose registers are more.
 constexpr int blocks_of_cu(int type_bytes, int dh, int waves) {
@@ -106,8 +113,9 @@ decode4_kernel(CacheView c, CacheScales sc4, AttendArgs a, DecodeScratch sc, int
   const TileRange tr = tile_range(len, a.window, a.sinks, true, TK);
   const int ns = WAVES == kDecodeWaves ? used_splits(tr.count, sc.nsplit) : 1;
   if (split >= ns) return;
-  const int t0 = static_cast<int>(static_cast<long long>(tr.count) * split / ns);
-  const int t1 = static_cast<int>(static_cast<long long>(tr.count) * (split + 1) / ns);
+  // (at most 2^19 tiles and kDecode4Blocks splits: their product is below 2^31)
+  const int t0 = static_cast<int>(static_cast<unsigned>(tr.count * split) / static_cast<unsigned>(ns));
+  const int t1 = static_cast<int>(static_cast<unsigned>(tr.count * (split + 1)) / static_cast<unsigned>(ns));
   const int head = qt * 16 + i16;                 // of the group
   const bool live = head < c.hg;
   const int hq = h * c.hg + head;
@@ -459,12 +467,6 @@ decode4_kernel(CacheView c, CacheScales sc4, AttendArgs a, DecodeScratch sc, int
 
 static int decode4_qtiles(const CacheView& c) { return (c.hg + 15) / 16; }
 
-// As many blocks as find room on the chip together, three to a CU (with two tiles
-// ahead, us with 512, 768, 1024 and 1536: 8 requests of 100000 to 131072 slots, 32 heads on
-// 8 of 128, 205, 200, 197 and 194; 64 of 200 to 4096, 28 on 4, 28.2, 26.3, 27.5 and 28; 16 of
-// them 13.0, 13.8, 15.4 and 17).  Splits of one length for all sequences, so that short ones
-// have fewer, were slower: 210 and 28.1.
-constexpr int kDecode4Blocks = 768;
 static int decode4_splits(const CacheView& c, int qtiles) {
   const long long groups = static_cast<long long>(c.n_seq) * c.hkv * qtiles;
   return used_splits((c.cap + kTile4 - 1) / kTile4, static_cast<int>((kDecode4Blocks + groups - 1) / groups));
