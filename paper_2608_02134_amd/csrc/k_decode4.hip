@@ -472,14 +472,25 @@ static int decode4_splits(const CacheView& c, int qtiles) {
   return used_splits((c.cap + kTile4 - 1) / kTile4, static_cast<int>((kDecode4Blocks + groups - 1) / groups));
 }
 
-// One block a head and no second kernel, as over pages of bf16.
-static bool decode4_short(const CacheView& c) {
-  const int tiles = (c.cap + kTile4 - 1) / kTile4;
-  return c.dh <= 128 && tiles > kDecodeWaves && tiles <= 2 * kDecodeShort;
+// One block of eight waves for a sequence's head and no second kernel, where a query
+// looks at few tiles: up to 20 of them (caches of up to four are one block of four waves
+// as it is), and more where the heads of all sequences are many, whose split parts cost
+// more than they spread.  GPU time in us so and split, 28 heads on 4 of 128 in bf16: 1
+// request of 640 slots 8.1 and 8.7, of 1024 10.3 and 8.7; 16 of 1024 10.5 and 10.6, of 2048
+// 16 and 13; 64 of 1024 12.1 and 16.6, of 2048 18.6 and 23.1, of 200 to 4096 28.9 and 24.7.
+// From kDecode4Blocks heads on nothing is split (256 of 640 22, so 32).
+static bool decode4_short(const CacheView& c, int window, int sinks) {
+  const long long heads = static_cast<long long>(c.n_seq) * c.hkv * decode4_qtiles(c);
+  const int all = (c.cap + kTile4 - 1) / kTile4;
+  long long seen = all;
+  if (window > 0) seen = std::min(seen, (static_cast<long long>(window) + sinks) / kTile4 + 3);   // (two runs of slots)
+  return c.dh <= 128 && all > kDecodeWaves && heads < kDecode4Blocks &&
+         seen <= std::min(64ll, std::max(20ll, heads / 2));
 }
 
 long long decode4_scratch_bytes(const CacheView& c) {
-  const int ns = decode4_short(c) ? 1 : decode4_splits(c, decode4_qtiles(c));
+  // (what is one block without a window is one with it)
+  const int ns = decode4_short(c, 0, 0) ? 1 : decode4_splits(c, decode4_qtiles(c));
   return ns == 1 ? 0 : 4ll * c.n_seq * c.hq * ns * (c.dh + 2);
 }
 
@@ -509,7 +520,7 @@ static hipError_t start_decode4(const CacheView& c, const CacheScales& s, const 
 hipError_t launch_cache4_decode(const CacheView& c, const CacheScales& s, const AttendArgs& a, void* scratch,
                                 hipStream_t st) {
   const int qt = decode4_qtiles(c);
-  const bool one_block = decode4_short(c);
+  const bool one_block = decode4_short(c, a.window, a.sinks);
   DecodeScratch sc{};
   sc.nsplit = one_block ? 1 : decode4_splits(c, qt);
   const bool join = sc.nsplit > 1;

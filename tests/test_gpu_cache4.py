@@ -202,11 +202,22 @@ def test_decode_lengths(window, page):
 
 
 @pytest.mark.parametrize("dtype,n", [("bf16", 4999), ("f32", 3001), ("bf16", 9000)])
-@pytest.mark.parametrize("window", [(0, 0), (700, 5)], ids=str)
+@pytest.mark.parametrize("window", [(0, 0), (700, 5), (100, 7), (1, 640), (4000, 2 ** 31 - 1)], ids=str)
 def test_decode_long(dtype, n, window):
     _say(f"decode4 long {dtype} n={n} window={window}")
     rng = np.random.default_rng(n)
     _decode(rng, C4.make(rng, dtype=dtype, hq=7, hkv=1, dh=128, page=128, lens=[n, n // 3], slots=n), *window)
+
+
+@pytest.mark.parametrize("n_seq,hkv,slots", [(16, 4, 1040), (64, 4, 330), (200, 4, 300), (256, 3, 160)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_decode_of_many_sequences(n_seq, hkv, slots, dtype):
+    """One block a head, of eight waves or four, and split ones, by the heads there are."""
+    _say(f"decode4 of {n_seq} sequences, {hkv} heads, {slots} slots {dtype}")
+    rng = np.random.default_rng(n_seq)
+    lens = rng.integers(0, slots + 1, n_seq).tolist()
+    _decode(rng, C4.make(rng, dtype=dtype, hq=hkv, hkv=hkv, dh=32, page=16, lens=lens, slots=slots), 0, 0)
+    _decode(rng, C4.make(rng, dtype=dtype, hq=hkv, hkv=hkv, dh=32, page=16, lens=lens, slots=slots), 70, 3)
 
 
 def test_decode_length_past_the_table_and_below_zero():
