@@ -135,7 +135,7 @@ def test_queries_in_place(n, dtype):
         assert C.same(C.host(x), C.rounded(O4.turn(q, r, 2 + np.arange(n)), dtype)), shape
 
 
-@pytest.mark.parametrize("n", [8, 9, 256, 257])
+@pytest.mark.parametrize("n", [4, 5, 8, 9, 256, 257])
 def test_few_and_many_tokens(n):
     """Tokens that one block takes, those whose heads four waves share and those that a
     wave has to itself: as one token at a time."""
