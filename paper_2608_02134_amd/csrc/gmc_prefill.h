@@ -487,7 +487,9 @@ __device__ __forceinline__ void prefill_block(const CacheView& c, const CacheSca
   // The run of the wave's unit u, and of its lane: whether it has a block (of V or
   // K), the block's row in the run and which of the row's it is.  Rows follow each
   // other by fours, as the chunks of r, r + 4, r + 8 and r + 12 stand on different
-  // banks.
+  // banks.  (Writes of four lanes with a row's blocks meet in pairs on a bank all the
+  // same, 256 cycles a tile; orders of lanes or chunks without that were no faster:
+  // 1012 and 991 us where this takes 994.)
   auto run_of = [&](int u) GMC_INLINE { return (w + kPreWaves * u) / kOfRun; };
   auto block_of = [&](int u, bool* value, int* r, int* blk) GMC_INLINE {
     const int x = 64 * ((w + kPreWaves * u) % kOfRun) + lane, y = x >= 16 * BR ? x - 16 * BR : x, at = y / BR;
