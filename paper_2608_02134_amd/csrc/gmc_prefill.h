@@ -705,7 +705,7 @@ __device__ __forceinline__ void prefill_block(const CacheView& c, const CacheSca
 }
 
 // Splits, grid and scratch memory of a call; the joining kernel where there are splits.
-PreScratch pre_plan(const CacheView& c, int max_new, bool four_bits, void* scratch, int* row_blocks);
+PreScratch pre_plan(const CacheView& c, const AttendArgs& a, bool four_bits, void* scratch, int* row_blocks);
 hipError_t launch_prefill_join(const CacheView& c, const AttendArgs& a, const PreScratch& sc, hipStream_t st);
 
 }  // namespace gmc

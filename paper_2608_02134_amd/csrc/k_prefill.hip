@@ -128,8 +128,8 @@ static int pre_row_blocks(const CacheView& c, int max_new) {
 // Over 4 bits also what a tile costs where two blocks share a CU (77 tokens over
 // 4100 slots 29.8 us with 240 blocks, 32.4 with 280; three such requests 43.7 with 480, 57
 // with 240; 16 over 32768 35.6 with 256, 38.6 with 348).
-static int pre_splits(const CacheView& c, int max_new, bool four_bits) {
-  const int kt = pre_key_tile(c, four_bits), tiles = (c.cap + kt - 1) / kt;
+static int pre_splits(const CacheView& c, int max_new, bool four_bits, int slots) {
+  const int kt = pre_key_tile(c, four_bits), tiles = (slots + kt - 1) / kt;
   const long long blocks = static_cast<long long>(pre_row_blocks(c, max_new)) * c.hkv * c.n_seq;
   const double tile = (c.dtype != 0 ? 1.7 / (64 * 128) : four_bits ? 3.0 / (64 * 128) : 1.9 / (32 * 64)) * kt * c.dh;
   const double part = 8e-6 / 4 * (c.dh + 2) * c.hq * max_new * c.n_seq;
@@ -147,14 +147,23 @@ static int pre_splits(const CacheView& c, int max_new, bool four_bits) {
 }
 
 long long prefill_scratch_bytes(const CacheView& c, int max_new, bool four_bits) {
-  const int ns = pre_splits(c, max_new, four_bits);
+  const int ns = pre_splits(c, max_new, four_bits, c.cap);
   return ns == 1 ? 0 : 4ll * c.n_seq * max_new * c.hq * ns * (c.dh + 2);
 }
 
-PreScratch pre_plan(const CacheView& c, int max_new, bool four_bits, void* scratch, int* row_blocks) {
+PreScratch pre_plan(const CacheView& c, const AttendArgs& a, bool four_bits, void* scratch, int* row_blocks) {
+  const int max_new = a.max_new;
   PreScratch sc{};
   *row_blocks = pre_row_blocks(c, max_new);
-  sc.nsplit = pre_splits(c, max_new, four_bits);
+  sc.nsplit = pre_splits(c, max_new, four_bits, c.cap);
+  // Under a window a block looks at few of the slots: splits for those, of the scratch
+  // memory that the capacity's splits need.  us so and with the capacity's: 43 tokens over
+  // 5488 slots, window 700, 18.5 and 20.4; three requests of 77 over 4100, 512, 24.0 and
+  // 27.6; 16 over 60000, 4096, 19.6 and 20.5; 300 over 32768, 1024, 33.0 and 32.4.
+  if (four_bits && a.window > 0) {
+    const long long slots = static_cast<long long>(a.window) + a.sinks + kPreRows / c.hg + 128;
+    if (slots < c.cap) sc.nsplit = std::min(sc.nsplit, pre_splits(c, max_new, true, static_cast<int>(slots)));
+  }
   if (sc.nsplit > 1) {
     sc.part = static_cast<float*>(scratch);
     sc.ml = sc.part + static_cast<long long>(c.n_seq) * max_new * c.hq * sc.nsplit * c.dh;
@@ -174,7 +183,7 @@ hipError_t launch_prefill_join(const CacheView& c, const AttendArgs& a, const Pr
 
 hipError_t launch_cache_prefill(const CacheView& c, const AttendArgs& a, void* scratch, hipStream_t st) {
   int row_blocks;
-  const PreScratch sc = pre_plan(c, a.max_new, false, scratch, &row_blocks);
+  const PreScratch sc = pre_plan(c, a, false, scratch, &row_blocks);
 #define GMC_PREFILL(T, DH)                                                                                       \
   case DH:                                                                                                       \
     hipLaunchKernelGGL((prefill_kernel<T, DH>), dim3(static_cast<unsigned>(sc.grid.blocks)), dim3(64 * kPreWaves), 0, st, c, a, sc, \

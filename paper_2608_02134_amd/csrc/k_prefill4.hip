@@ -21,7 +21,7 @@ prefill4_kernel(CacheView c, CacheScales s, AttendArgs a, PreScratch sc, int row
 hipError_t launch_cache4_prefill(const CacheView& c, const CacheScales& s, const AttendArgs& a, void* scratch,
                                  hipStream_t st) {
   int row_blocks;
-  const PreScratch sc = pre_plan(c, a.max_new, true, scratch, &row_blocks);
+  const PreScratch sc = pre_plan(c, a, true, scratch, &row_blocks);
 #define GMC_PREFILL4(T, DH)                                                                                       \
   case DH:                                                                                                        \
     hipLaunchKernelGGL((prefill4_kernel<T, DH>), dim3(static_cast<unsigned>(sc.grid.blocks)), dim3(64 * kPreWaves), 0, st, \

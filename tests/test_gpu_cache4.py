@@ -272,6 +272,15 @@ def test_prefill_long(dtype, window):
     _prefill(rng, c, [900, 333], *window)
 
 
+@pytest.mark.parametrize("window", [(1, 0), (130, 4), (700, 1), (3900, 9), (9, 2 ** 31 - 1), (2 ** 31 - 1, 2 ** 31 - 1)], ids=str)
+def test_prefill_window_of_long_caches(window):
+    """Windows far below the capacity: fewer splits than the scratch memory is for."""
+    _say(f"prefill4 windows of long caches {window}")
+    rng = np.random.default_rng(32)
+    c = C4.make(rng, dtype="bf16", hq=7, hkv=1, dh=64, page=64, lens=[4100, 2055], slots=5000)
+    _prefill(rng, c, [43, 9], *window)
+
+
 def test_prefill_more_rows_than_slots_held():
     """Queries that stand before the first slot see nothing."""
     _say("prefill4 before the first slot")
