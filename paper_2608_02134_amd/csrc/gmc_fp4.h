@@ -59,20 +59,22 @@ __device__ __forceinline__ void split3(float x, __bf16* part) {
   part[2] = static_cast<__bf16>(rest - __uint_as_float(v));
 }
 
-// A weight (not negative) as two or three parts, none of which is zero if it is
-// not: an infinite value, which scales from 2^126 on have, stays what it is.
+// A weight (not negative) as two or three parts.  An infinite value, which scales from
+// 2^126 on have, times a part of zero would be NaN: no part of a weight that is not zero
+// is below the least bf16, 2^-133, which is under 2^-17 and 2^-25 of weights down to 2^-116
+// and 2^-108.  (Weights below 2^-126 of the largest are zero as a whole in 32 bits.)
 __device__ __forceinline__ void split2_weight(float e, __bf16* part) {
   const uint32_t u = __float_as_uint(e) & 0xFFFF0000u;
   part[0] = upper_half(u);
-  part[1] = static_cast<__bf16>(fmaxf(e - __uint_as_float(u), e * 0x1p-24f));
+  part[1] = static_cast<__bf16>(fmaxf(e - __uint_as_float(u), fminf(e, 0x1p-133f)));
 }
 __device__ __forceinline__ void split3_weight(float e, __bf16* part) {
   const uint32_t u = __float_as_uint(e) & 0xFFFF0000u;
-  const float rest = e - __uint_as_float(u);
-  const uint32_t v = __float_as_uint(fmaxf(rest, e * 0x1p-25f)) & 0xFFFF0000u;
+  const float rest = e - __uint_as_float(u), least = fminf(e, 0x1p-133f);
+  const uint32_t v = __float_as_uint(fmaxf(rest, least)) & 0xFFFF0000u;
   part[0] = upper_half(u);
   part[1] = upper_half(v);
-  part[2] = static_cast<__bf16>(fmaxf(rest - __uint_as_float(v), e * 0x1p-33f));
+  part[2] = static_cast<__bf16>(fmaxf(rest - __uint_as_float(v), least));
 }
 
 }  // namespace gmc

@@ -630,3 +630,41 @@ def test_wrapper_on_the_device():
     f32 = C4.on_gpu({**c, "dtype": "f32"})
     out = f32.decode(x[:2].float())
     assert out.dtype == torch.float32
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("below", [70, 75, 80, 87])
+@pytest.mark.parametrize("slots,one,other", [(208, 3, 5), (208, 3, 150), (1328, 40, 1100), (1328, 900, 700)])
+def test_infinite_values_of_small_weights(dtype, below, slots, one, other):
+    """An infinite value on a key whose logit is `below` under the largest, so that its
+    weight is small but no less than 2^-126: no part of that weight may vanish."""
+    _say(f"4 bits, infinite values of small weights {dtype} {below} {slots} {one} {other}")
+    rng = np.random.default_rng(below)
+    n, dh = slots - 8, 96
+    c = C4.make(rng, dtype=dtype, hq=4, hkv=2, dh=dh, page=16, lens=[n], slots=slots)
+    row = lambda s: (c["table"][0][s // 16], slice(None), s % 16)  # noqa: E731
+    for s in range(n):
+        c["k_codes"][row(s)] = 0
+    # products with queries of one: `below` for the other key, 0 for all besides
+    c["k_codes"][row(other)][:, :below] = 2
+    c["k_scales"][row(other)] = 127
+    d = {0: (5, 7, np.inf), 1: (70, 15, -np.inf)}       # of each kv head: dimension, code, what it reads as
+    for h, (at, code, _) in d.items():
+        page, _, r = row(one)
+        c["v_codes"][page, h, r, 32 * (at // 32):32 * (at // 32) + 32] = 0
+        c["v_codes"][page, h, r, at] = code
+        c["v_scales"][page, h, r, at // 32] = 254
+    C4.refresh(c)
+    q = C.to_gpu(np.ones((1, 4, dh)), dtype)
+    dev = C4.on_gpu(c)
+    want = np.repeat(c["v"][row(other)], 2, 0)[None]
+    for what, out in (("decode", dev.decode(q, scale=1.0)), ("prefill", dev.prefill(q, scale=1.0))):
+        out = C.host(out)
+        for h in range(4):
+            at, _, inf = d[h // 2]
+            assert out[0, h, at] == inf, (what, h, out[0, h, at])
+            rest = np.arange(dh) != at
+            # the weight of `other` is 1 but for roundings of weight, product, quotient and
+            # output; what the rest add is below 1400 e^-70 6
+            tol = (3 * C.UBF if dtype == "bf16" else 16 * C.U32) * np.abs(want[0, h]) + 1e-26
+            assert (np.abs(out[0, h] - want[0, h]) <= tol)[rest].all(), (what, h)
