@@ -45,18 +45,21 @@ __device__ __forceinline__ uint32_t fp4_codes(const float* x, float scale) {
 }
 
 // fp32 beside values of 4 bits, which are bf16: x as the upper 8 significant bits,
-// the next 8, and the rest rounded.  Infinities and NaN are all in the first part.
+// the next 8, and the rest rounded; infinities and NaN in the first.
+// An infinite value, which scales from 2^126 on have, times a part of zero would be NaN:
+// the least bf16, 2^-133, with x's sign is added to the second and third part.
 __device__ __forceinline__ __bf16 upper_half(uint32_t u) {
   return __builtin_bit_cast(__bf16, static_cast<uint16_t>(u >> 16));
 }
 __device__ __forceinline__ void split3(float x, __bf16* part) {
   const uint32_t u = __float_as_uint(x);
   const bool finite = (u & 0x7F800000u) != 0x7F800000u;
-  const float rest = finite ? x - __uint_as_float(u & 0xFFFF0000u) : 0.f;
+  const float least = __builtin_amdgcn_fmed3f(x, -0x1p-133f, 0x1p-133f);   // (0 for x = 0)
+  const float rest = (finite ? x - __uint_as_float(u & 0xFFFF0000u) : 0.f) + least;
   const uint32_t v = __float_as_uint(rest) & 0xFFFF0000u;
   part[0] = finite ? upper_half(u) : static_cast<__bf16>(x);
   part[1] = upper_half(v);
-  part[2] = static_cast<__bf16>(rest - __uint_as_float(v));
+  part[2] = static_cast<__bf16>(rest - __uint_as_float(v) + least);
 }
 
 // A weight (not negative) as two or three parts.  An infinite value, which scales from

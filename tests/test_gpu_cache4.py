@@ -668,3 +668,53 @@ def test_infinite_values_of_small_weights(dtype, below, slots, one, other):
             # output; what the rest add is below 1400 e^-70 6
             tol = (3 * C.UBF if dtype == "bf16" else 16 * C.U32) * np.abs(want[0, h]) + 1e-26
             assert (np.abs(out[0, h] - want[0, h]) <= tol)[rest].all(), (what, h)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dh", [64, 160, 224])
+def test_keys_that_overflow(dh, dtype):
+    """An infinity among K's values makes an infinite logit with the product's sign:
+    the key is not seen where that is negative, the row is NaN where it is positive."""
+    _say(f"4 bits, infinite keys dh={dh} {dtype}")
+    rng = np.random.default_rng(dh + 2)
+    c = C4.make(rng, dtype=dtype, hq=4, hkv=2, dh=dh, page=16, lens=[100, 77], slots=112)
+    for b, h, s, at, code in ((0, 0, 70, 5, 15), (1, 1, 50, dh - 1, 7)):
+        page, r = c["table"][b][s // 16], s % 16
+        c["k_codes"][page, h, r, 32 * (at // 32):32 * (at // 32) + 32] = 0
+        c["k_codes"][page, h, r, at] = code
+        c["k_scales"][page, h, r, at // 32] = 254
+    C4.refresh(c)
+    with np.errstate(over="ignore"):
+        c["k"] = c["k"].astype(np.float32).astype(np.float64)
+    new = [60, 60]
+    # few bits, so that an fp32 query is one bf16 alone; no zeros
+    q = rng.choice([-2.0, -1.5, -0.5, 0.5, 1.0, 1.75], (sum(new), 4, dh))
+    dev = C4.on_gpu(c)
+    x = C.to_gpu(q, dtype)
+    for (out, lse), first, n, decode in ((dev.prefill(x, lse=True), [0, 60], new, False),
+                                         (dev.decode(x[[59, 119]], lse=True), [0, 1], [1, 1], True)):
+        rows = q if not decode else q[[59, 119]]
+        with np.errstate(invalid="ignore"):
+            ref = O.attend(c, rows, first, n, dh ** -0.5)
+        _finite_as_formula(ref, C.host(out), C.host(lse), dtype, dh, decode)
+
+
+def _finite_as_formula(ref, out, lse, dtype, dh, decode):
+    """NaN where the formula has it and the other elements within C4.check_attention's
+    bounds, element by element.  (Sizes of infinite products bound nothing: as of the others.)"""
+    assert np.array_equal(np.isnan(out), np.isnan(ref["out"])) and np.array_equal(np.isnan(lse), np.isnan(ref["lse"]))
+    assert np.isfinite(ref["out"]).any() and np.isnan(ref["out"]).any()
+    _elements(ref, out, lse, dtype, dh, decode)
+
+
+def _elements(ref, out, lse, dtype, dh, decode, lost=0.0):
+    """C4.check_attention's bounds for each element that is finite, `lost` beside them."""
+    terms = 3 if dtype == "f32" else 2 if decode else 1
+    size = np.where(np.isfinite(ref["size"]), ref["size"], np.nanmax(ref["size"][np.isfinite(ref["size"])]))
+    rel = C.weight_error({"size": size, "most": ref["most"] * terms}, dh if dtype == "bf16" else dh * terms)
+    live, seen = np.isfinite(ref["out"]), np.isfinite(ref["lse"])
+    step = C.UBF * 1.01 if dtype == "bf16" else 0.0
+    with np.errstate(invalid="ignore"):
+        tol = ref["mass"] * (rel[..., None] + step) + (step + C.U32) * np.abs(ref["out"]) + lost
+        assert (np.abs(out - ref["out"]) <= tol)[live].all()
+        assert (np.abs(lse - ref["lse"]) <= rel + 2 * C.U32 * np.abs(ref["lse"]))[seen].all()
