@@ -718,3 +718,71 @@ def _elements(ref, out, lse, dtype, dh, decode, lost=0.0):
         tol = ref["mass"] * (rel[..., None] + step) + (step + C.U32) * np.abs(ref["out"]) + lost
         assert (np.abs(out - ref["out"]) <= tol)[live].all()
         assert (np.abs(lse - ref["lse"]) <= rel + 2 * C.U32 * np.abs(ref["lse"]))[seen].all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dh", [64, 96, 160, 256])
+def test_elements_beside_blocks_of_nan(dh, dtype):
+    """What is beside a NaN - other blocks of its row, other heads, other tokens - is
+    as the formula has it, element by element."""
+    _say(f"4 bits, beside blocks of NaN dh={dh} {dtype}")
+    rng = np.random.default_rng(dh + 3)
+    c = C4.make(rng, dtype=dtype, hq=6, hkv=3, dh=dh, page=16, lens=[100, 77], slots=112)
+    for b, h, s, blk, x in ((0, 0, 70, 0, "v"), (0, 1, 90, dh // 32 - 1, "v"), (1, 0, 60, 1, "k"), (1, 2, 5, 0, "v")):
+        c[x + "_scales"][c["table"][b][s // 16], h, s % 16, blk] = 255
+    C4.refresh(c)
+    new = [60, 77]
+    q = C.queries(rng, c, sum(new))
+    dev, x = C4.on_gpu(c), C.to_gpu(q, dtype)
+    for window in ((0, 0), (20, 2)):
+        for (out, lse), first, n, rows in ((dev.prefill(x, starts=_starts(new), max_new=77, window=window[0],
+                                                        sinks=window[1], lse=True), [0, 60], new, q),
+                                           (dev.decode(x[:2], window=window[0], sinks=window[1], lse=True), [0, 1],
+                                            [1, 1], q[:2])):
+            with np.errstate(invalid="ignore"):
+                ref = O.attend(c, rows, first, n, dh ** -0.5, *window)
+            _finite_as_formula(ref, C.host(out), C.host(lse), dtype, dh, len(rows) == 2)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dh", [32, 64, 96, 256])
+def test_prefill_over_scales_of_every_size(dh, dtype):
+    """Scales of K and V from the least on; products and sums of fp32 hold the largest."""
+    _say(f"prefill4, scales of every size dh={dh} {dtype}")
+    rng = np.random.default_rng(15)
+    new = [20, 33]
+    for low, high in ((30, 240), (100, 150), (0, 30)):
+        c = C4.make(rng, dtype=dtype, hq=4, hkv=2, dh=dh, page=16, lens=[60, 33], slots=64)
+        live = c["v_scales"] != 255
+        c["v_scales"][live] = rng.integers(low, high, live.sum())
+        C4.refresh(c)
+        if low:
+            _prefill(rng, c, new, 0, 0)
+            continue
+        # below the least normal number: each of up to 60 keys' three products, the
+        # quotient and the output may lose what is below 2^-126
+        _both(rng, c, new, None, 182 * 2.0 ** -126, decode=False)
+    for low, high, scale in ((0, 30, 1.0), (215, 222, 2.0 ** -95)):
+        c = C4.make(rng, dtype=dtype, hq=4, hkv=2, dh=dh, page=16, lens=[60, 33], slots=64)
+        live = c["k_scales"] != 255
+        c["k_scales"][live] = rng.integers(low, high, live.sum())
+        C4.refresh(c)
+        # (logits lie up to 200 apart: a weight below 2^-126 of the largest is zero in 32
+        # bits, so each of 60 keys may lose 2^-126 of a value of up to 6 / 2.  With heads of 256
+        # all keys whose value is not zero are such ones for a query, whose element is 1e-39)
+        _both(rng, c, new, scale, 180 * 2.0 ** -126)
+
+
+def _both(rng, c, new, scale, lost, decode=True):
+    """Prefill of the new tokens, and decode of other queries, within _elements' bounds."""
+    dtype, dh = c["dtype"], c["k"].shape[3]
+    scale = dh ** -0.5 if scale is None else scale
+    first = np.concatenate([[0], np.cumsum(new)])
+    q = C.queries(rng, c, first[-1])
+    dev, x = C4.on_gpu(c), C.to_gpu(q, dtype)
+    out, lse = dev.prefill(x, starts=_starts(new), max_new=max(new), scale=scale, lse=True)
+    _elements(O.attend(c, q, first, new, scale), C.host(out), C.host(lse), dtype, dh, False, lost)
+    if decode:
+        q = C.queries(rng, c, 2)
+        out, lse = dev.decode(C.to_gpu(q, dtype), scale=scale, lse=True)
+        _elements(O.attend(c, q, [0, 1], [1, 1], scale), C.host(out), C.host(lse), dtype, dh, True, lost)
