@@ -786,3 +786,37 @@ def _both(rng, c, new, scale, lost, decode=True):
         q = C.queries(rng, c, 2)
         out, lse = dev.decode(C.to_gpu(q, dtype), scale=scale, lse=True)
         _elements(O.attend(c, q, [0, 1], [1, 1], scale), C.host(out), C.host(lse), dtype, dh, True, lost)
+
+
+def test_refused_calls_leave_the_cache():
+    _say("4 bits, what refused calls leave")
+    rng = np.random.default_rng(16)
+    c = C4.make(rng, dtype="bf16", hq=4, hkv=2, dh=64, page=16, lens=[20, 5], slots=32)
+    dev, full = C4.on_gpu(c), C.on_gpu(C.make(rng, dtype="bf16", hq=4, hkv=2, dh=64, page=16, lens=[20, 5], slots=32,
+                                              positions=True, weights=True))
+    held = ("lens", "page_table", "k_codes", "v_codes", "k_scales", "v_scales", "k_pages", "v_pages", "seen",
+            "slot_pos", "weights")
+    bits = lambda t: t.clone().view(torch.uint8)  # noqa: E731
+    before = [{x: bits(getattr(cache, x)) for x in held if getattr(cache, x, None) is not None} for cache in (dev, full)]
+    x = torch.ones((4, 8, 64), dtype=torch.bfloat16, device="cuda")
+    q, k, v = x[:, :4], x[:, 4:6], x[:, 6:]
+    r = C4.rotary_on_gpu(C4.rotary(rng, 8, 64))
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32, device="cuda")  # noqa: E731
+    for cache in (dev, full):
+        big = x.repeat(20, 1, 1)
+        for refused in (lambda: cache.append(big[:, 4:6], big[:, 6:]), lambda: cache.append(k, v[:3]),
+                        lambda: cache.append(k.float(), v), lambda: cache.append(k, v, starts=i32(3)),
+                        lambda: cache.append(k, v, src=i32(2, 40)), lambda: cache.append(k, v, src=i32(3, 1)),
+                        lambda: cache.append_rotary(k, v, r, pos=i32(3)),
+                        lambda: cache.append_rotary(k, v, r, q=q[:3]),
+                        lambda: cache.append_rotary(k, v, r, q=q, out=torch.empty_like(q)[:3]),
+                        lambda: cache.append_rotary(k, v, B.Rotary.create(4, 128)),
+                        lambda: cache.append_rotary(big[:, 4:6], big[:, 6:], r),
+                        lambda: cache.decode(x[:3, :4]), lambda: cache.prefill(q.float()),
+                        lambda: cache.evict(1, sinks=1, recent=1)):
+            with pytest.raises((ValueError, TypeError, RuntimeError)):
+                refused()
+    torch.cuda.synchronize()
+    for cache, was in zip((dev, full), before):
+        for name, t in was.items():
+            assert torch.equal(bits(getattr(cache, name)), t), name
