@@ -685,7 +685,10 @@ typedef struct gmc_rotary {
  *           of k (with src: of each row that is picked from, as
  *           gmc_compact_sequence leaves a sequence's).  NULL: the position that
  *           the slot gets, seen[b] + i, or lens[b] + i in a cache without seen,
- *           for all of t, h and w
+ *           for all of t, h and w.  That is a token's position only where the rows
+ *           before it stand at theirs: behind a prompt of which src took some
+ *           rows, or whose (t,h,w) are not its rows' indices, text goes on behind
+ *           the whole prompt's largest position, and pos has to say so
  *   q       rows of n_q_heads * head_dim elements, q_stride elements apart, one
  *           for each row of k; NULL: no queries (q_out is NULL too)
  *   q_out   [n][n_q_heads][head_dim] dtype, 16-byte aligned: the rotated query of

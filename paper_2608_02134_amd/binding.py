@@ -911,7 +911,8 @@ class KvCache:
     def append_rotary(self, k, v, rotary, *, pos=None, q=None, starts=None, max_new=None, src=None, out=None):
         """gmc_cache_append_rotary: append with k rotated by ``rotary`` (a Rotary)
         on the way.  ``pos`` int32 [tokens], or [tokens][3] where the rotary has
-        sections; None: the slots' positions.  ``q`` [tokens][n_q_heads][head_dim]:
+        sections; None: the slots' positions, which are not those of an answer to a
+        pruned prompt (see gmc_cache_append_rotary).  ``q`` [tokens][n_q_heads][head_dim]:
         the tokens' queries; their rotated ones are returned (in ``out`` if given,
         which without src may be q), [n_seq * n][n_q_heads][head_dim] with src."""
         rows = self._appended(k, v, starts, max_new, src)
