@@ -762,7 +762,8 @@ class Rotary:
     @classmethod
     def create(cls, n_pos, rot_dim, *, base=10000.0, device="cuda", **more):
         """The angles position * base ** (-2 j / rot_dim) of pairs j, formed in
-        64 bits (at position 10^5 the first pair's would be off by 4e-3 in 32)."""
+        64 bits (in 32 their rounding alone is up to 4e-3 from 2^16 on, which
+        the second pair's reaches at position 10^5)."""
         import torch
         if n_pos < 1 or rot_dim < 16 or rot_dim % 16 != 0:
             raise ValueError(f"n_pos={n_pos} must be at least 1 and rot_dim={rot_dim} a positive multiple of 16")

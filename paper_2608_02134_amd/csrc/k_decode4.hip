@@ -88,7 +88,8 @@ template <int N> __device__ __forceinline__ void arrive() {   // until at most N
 // ahead, us with 512, 768, 1024 and 1536: 8 requests of 100000 to 131072 slots, 32 heads on
 // 8 of 128, 205, 200, 197 and 194; 64 of 200 to 4096, 28 on 4, 28.2, 26.3, 27.5 and 28; 16 of
 // them 13.0, 13.8, 15.4 and 17).  Splits of one length for all sequences, so that short ones
-// have fewer, were slower: 210 and 28.1.
+// have fewer, were slower: 210 and 28.1.  Wider heads, whose CUs hold two blocks or one
+// (blocks_of_cu), have the same number; others were not measured for them.
 constexpr int kDecode4Blocks = 768;
 
 // Three blocks of four waves to a CU with heads of up to 128, two with wider ones and

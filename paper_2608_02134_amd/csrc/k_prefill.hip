@@ -118,8 +118,11 @@ static int pre_row_blocks(const CacheView& c, int max_new) {
 
 // Splits of a row block's keys, while the blocks find room on the chip together
 // (512): a block's tiles, one after the other, against a second launch and the
-// parts it reads.  Estimates in us: a tile 1.7 for 64 keys of 128 dims (fp32:
-// 1.9 for 32 of 64), the launch 4, parts 4 MB each.  Measured, us with the splits
+// parts it reads.  512 is two to a CU, as kernels of up to 256 registers have it: bf16 with
+// heads of up to 128, fp32 up to 64 over pages and 32 over 4 bits.  Of the others a CU holds
+// one, and blocks from 257 on wait; another limit was not measured for them.  Estimates
+// in us: a tile 1.7 for 64 keys of 128 dims (fp32: 1.9 for 32 of 64), the launch 4,
+// parts 4 MB each.  Measured, us with the splits
 // chosen and with others: 335 tokens (28 query heads on 4 of 128) 16.7 with 1,
 // 20.7 with 2; 1000 tokens 32.5 with 1, 41 with 2; 77 tokens over 4100 slots 27.9
 // with 16, 26.2 with 10, 29.8 with 25; 10 over 2000 14.1 with 15, 19.6 with 5;
@@ -159,7 +162,8 @@ PreScratch pre_plan(const CacheView& c, const AttendArgs& a, bool four_bits, voi
   // Under a window a block looks at few of the slots: splits for those, of the scratch
   // memory that the capacity's splits need.  us so and with the capacity's: 43 tokens over
   // 5488 slots, window 700, 18.5 and 20.4; three requests of 77 over 4100, 512, 24.0 and
-  // 27.6; 16 over 60000, 4096, 19.6 and 20.5; 300 over 32768, 1024, 33.0 and 32.4.
+  // 27.6; 16 over 60000, 4096, 19.6 and 20.5; 300 over 32768, 1024, 33.0 and 32.4.  (Over
+  // pages of the type it was not measured, and the capacity's stand.)
   if (four_bits && a.window > 0) {
     const long long slots = static_cast<long long>(a.window) + a.sinks + kPreRows / c.hg + 128;
     if (slots < c.cap) sc.nsplit = std::min(sc.nsplit, pre_splits(c, max_new, true, static_cast<int>(slots)));

@@ -106,7 +106,9 @@ __device__ __forceinline__ uint32_t block_top(const float* x) {
 // One token: heads of K, V and q, 64 / (dh / 8) at a time to a wave, by `parts`
 // waves of which this is number `part`.  s: its slot (one past the capacity is not
 // stored); from: its row in k, v, q and pos; to: in q_out.  (The first heads' loads
-// before the position's and the page's: 69 us where this takes 62 for 16448 tokens.)
+// before the position's and the page's, us with the launches around it: 66 where this
+// takes 61 for 16448 tokens; 16 prompts of 335 picked rows into 4 bits and read back 19.7
+// and 19.5; one token of 16 sequences 6.6 and 6.4.)
 template <typename T, bool Q4, int PAIRS>
 __device__ __forceinline__ void append_turned(const CacheView& c, const CacheScales& sc, const RotaryView& r,
                                               const RotaryArgs& a, int b, int s, int position, long long from,
