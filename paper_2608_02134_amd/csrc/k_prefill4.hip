@@ -10,7 +10,7 @@
 // on 4 of 128, 0.63 ms; products of fp32 took 1.82.  bf16 weights are rounded to bf16 once
 // for the second product, as over pages of bf16 (and not as in decode, which has the
 // matrix cores to spare for two parts): the outputs' error against 64 bits, relative to
-// their size, is 0.0020 to 0.0022, where two parts of each weight have the 0.0016 of the
+// their size, is 0.0018 to 0.0022, where two parts of each weight have the 0.0016 of the
 // output's own rounding and take 1.28 ms for the 16448 tokens where this takes 1.00.
 #include "gmc_prefill.h"
 
